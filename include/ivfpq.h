@@ -323,6 +323,125 @@ int ivfpq_probe_static(const ivfpq_index_t* index, const float* queries, int64_t
  * the word. */
 int ivfpq_static_status(void* stream);
 
+/* ---- key/value cache: attention as a search over the keys ------------------------------------
+ * The paper's closing discussion treats a language model's attention as the same similarity search:
+ * the query's inner products with all keys, of which a small part carries the result.  These entry
+ * points are that search over a paged key/value cache: the inverted lists become pages (blocks) of
+ * `page` tokens, filtering becomes a cheap score per block from 8-bit bounds of its keys, the codes
+ * become keys and values held in 4 bits (or 16), and the scan ends in a softmax instead of a top-k.
+ *
+ * Formats.  IVFPQ_KV_BF16 / IVFPQ_KV_FP16: keys and values [npages][nheads][page][d] with any strides
+ * (multiples of 8 elements; the d elements of a token and head contiguous and 16-byte aligned).
+ * IVFPQ_KV_INT4: one array of records [npages][nheads][page / 16][18 * d bytes], 16-byte aligned;
+ * a record holds 16 tokens.  A token's d elements are in groups of 64 with a 16-bit scale s and
+ * offset z each; a code u in 0..15 stands for s * u + z.  Quantizer, in fp32 on x clamped to +-65504
+ * (NaN has an unspecified code): z = fp16(min), s = fp16((max - z) * (1 / 15)),
+ * u = rint((x - z) / s) clamped to 0..15, u = 0 where s = 0.  Record, with planes p of D = min(d, 128) elements, the lower nibble of a byte first:
+ *   keys              [p][token 16][c 4][group][half 2][nibble 8]: element 64 group + 16 c + 8 half + nibble
+ *   values            [p][octet 2][r 8][c 4][parity 2][nibble D/8]: token 8 octet + 2 c + parity,
+ *                     element D/8 r + nibble
+ *   key parameters    fp16 [token 16][group of d][s, z]
+ *   value parameters  fp16 [octet 2][group of d][c 4][s, s, z, z of parity 0, 1]
+ * Block bounds (optional; for ivfpq_kv_select): bounds int8 [npages][nheads][2][d] and bounds_scale fp32
+ * [npages][nheads]: when a page has become full, per channel the largest and the smallest of its held
+ * key values x as rint(x * (127 * (1 / top))), top the largest magnitude among them, and scale
+ * top * (1 / 127) (fp32, every step rounded).
+ *
+ * A batch is nreq requests.  Request r holds seq_len[r] tokens (those of this call included) in the pages
+ * block_table[r * table_stride + 0, 1, ...]; its new tokens are rows q_start[r] .. q_start[r + 1] - 1 of the
+ * call's ntok rows and have the last positions.  q_start NULL: one token per request, ntok = nreq.  A token whose
+ * position would be negative (an unused slot: seq_len 0) is not written, sees nothing and lists nothing.
+ * Array contents are device memory that the library cannot check on the host: a page outside the cache, a
+ * request longer than its table row or decreasing q_start is met by skipping the access and raising the
+ * status flag of the workspace.
+ *
+ * Workspace: dev, 256-byte aligned, ivfpq_kv_workspace_bytes; its first IVFPQ_KV_WORKSPACE_ZERO bytes zeroed ONCE by
+ * the caller before its first use (every call leaves them zeroed but for the status word).  Calls whose kernels may
+ * overlap need workspaces of their own.  All calls are asynchronous on `stream`, allocate nothing and can be
+ * captured in CUDA graphs.  d = 64, 128 or 256; page = 16, 32, 64 or 128; nreq, ntok <= 2^20; nheads <= 1024,
+ * IVFPQ_KV_MAX_GROUP query heads per kv head. */
+#define IVFPQ_KV_INT4 0
+#define IVFPQ_KV_BF16 1
+#define IVFPQ_KV_FP16 2
+#define IVFPQ_KV_MAX_SELECT 1024
+#define IVFPQ_KV_MAX_GROUP 64
+#define IVFPQ_KV_MAX_BLOCKS 32768
+#define IVFPQ_KV_WORKSPACE_ZERO 8192
+
+typedef struct {
+    int32_t format;         /* IVFPQ_KV_*                                                             */
+    int32_t d;              /* head width: 64, 128 or 256                                             */
+    int32_t nheads;         /* key/value heads                                                        */
+    int32_t page;           /* tokens per page: 16, 32, 64 or 128                                     */
+    int64_t npages;
+    void* k;                /* dev, 16-bit formats: keys (page, head and token strides in elements)   */
+    void* v;
+    int64_t k_stride[3];
+    int64_t v_stride[3];
+    void* records;          /* dev, IVFPQ_KV_INT4                                                     */
+    int8_t* bounds;         /* dev or NULL (no bounds are kept, ivfpq_kv_select refused)              */
+    float* bounds_scale;
+} ivfpq_kv_cache_t;
+
+typedef struct {
+    int32_t nreq;
+    int32_t max_blocks;         /* columns of the block table (ivfpq_kv_select: <= IVFPQ_KV_MAX_BLOCKS)   */
+    int64_t table_stride;       /* elements between its rows                                           */
+    const int32_t* block_table; /* dev                                                                 */
+    const int32_t* seq_len;     /* dev [nreq]                                                          */
+    const int32_t* q_start;     /* dev [nreq + 1] or NULL                                              */
+} ivfpq_kv_batch_t;
+
+/* Bytes of workspace that any call on caches of head width d needs (0: no such width). */
+size_t ivfpq_kv_workspace_bytes(int32_t d);
+
+/* Writes the batch's new keys and values (dev, 16-bit `dtype`: IVFPQ_KV_BF16 or IVFPQ_KV_FP16, equal to a
+ * 16-bit cache's format; [ntok][nheads][d], token and head strides in elements, multiples of 8, 16-byte aligned) to their
+ * places and, where bounds are kept, the bounds of every page that they fill up. */
+int ivfpq_kv_append(const ivfpq_kv_cache_t* cache, const ivfpq_kv_batch_t* batch, int64_t ntok, int32_t dtype,
+                    const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
+                    int64_t v_token_stride, int64_t v_head_stride, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/* Reads the held values of the batch's tokens back: k_out, v_out dev [ntok][nheads][d] of `dtype`, 16-byte
+ * aligned (zeros for a token of negative position). */
+int ivfpq_kv_read(const ivfpq_kv_cache_t* cache, const ivfpq_kv_batch_t* batch, int64_t ntok, int32_t dtype,
+                  void* k_out, void* v_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The bounds of n physical pages (dev) as the values they stand for, code * scale: upper, lower
+ * dev fp32 [n][nheads][d], 16-byte aligned (zeros for a page outside the cache, which raises the flag). */
+int ivfpq_kv_read_bounds(const ivfpq_kv_cache_t* cache, const int32_t* pages, int64_t n, float* upper, float* lower,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* Filtering: for every token and kv head the nselect blocks to attend over, blocks_out dev int32
+ * [ntok][nheads][nselect], ascending, padded with -1.  A token at position p sees blocks 0 .. p / page.  The first nsink and
+ * the last nlocal (>= 1: the token's own block need not be full) of them are always listed, the others in the order
+ * of (score descending, block ascending):
+ *   score = bounds_scale * max over the kv head's query heads of sum_i max(q8_i * upper8_i, q8_i * lower8_i),
+ *   q8 = rint(q * (127 * (1 / largest |q| of the kv head's query heads))),
+ * an upper bound of the block's logits up to rounding.  Whole numbers, one fp32 product: the same lists whatever
+ * the order of summation.  A NaN score ranks last.  q dev [ntok][nheads * group][d] of `dtype` (strides as above;
+ * query head h belongs to kv head h / group, nq_heads = nheads * group), nsink + nlocal <= nselect <= IVFPQ_KV_MAX_SELECT. */
+int ivfpq_kv_select(const ivfpq_kv_cache_t* cache, const ivfpq_kv_batch_t* batch, int64_t ntok, int32_t dtype,
+                    const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t nq_heads, int32_t nselect,
+                    int32_t nsink, int32_t nlocal, int32_t* blocks_out, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/* Attention of the batch's tokens over the keys at positions <= their own: all of them (blocks NULL) or
+ * those in the blocks listed for the token and kv head (dev int32 [ntok][nheads][nselect], distinct; entries outside
+ * 0 .. p / page are passed over).  out[t][h] = sum_j softmax_j(scale * q.k_j) v_j of `dtype`, dev [ntok][nq_heads][d]
+ * contiguous, 16-byte aligned; lse (dev fp32 [ntok][nq_heads] or NULL) = log sum_j exp(scale * q.k_j).  A row that sees no key: zeros and
+ * -inf.  The keys and values of positions beyond a token's own are not used, whatever bits they hold.  dtype equals a 16-bit
+ * cache's format.  Sums and softmax statistics are fp32. */
+int ivfpq_kv_attend(const ivfpq_kv_cache_t* cache, const ivfpq_kv_batch_t* batch, int64_t ntok, int32_t dtype,
+                    const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t nq_heads, float scale,
+                    const int32_t* blocks, int32_t nselect, void* out, float* lse, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
+/* Synchronises `stream`, reports and clears the status word of the calls that used `workspace`:
+ * IVFPQ_OK, IVFPQ_ERR_DEVICE_FLAG or IVFPQ_ERR_CUDA. */
+int ivfpq_kv_status(void* workspace, void* stream);
+
 const char* ivfpq_error_string(int code);
 
 /* ---- test-only exports (small inputs) -------------------------------------------------------

@@ -48,6 +48,9 @@ EXPORTS = (
     "ivfpq_debug_probes", "ivfpq_debug_search", "ivfpq_probe_static", "ivfpq_static_status", "ivfpq_query_thresholds",
     "ivfpq_query_thresholds_knn",
     "ivfpq_entry_stats",
+    # key/value cache (kv.py)
+    "ivfpq_kv_workspace_bytes", "ivfpq_kv_append", "ivfpq_kv_read", "ivfpq_kv_read_bounds", "ivfpq_kv_select",
+    "ivfpq_kv_attend", "ivfpq_kv_status",
 )
 
 

@@ -1,0 +1,174 @@
+// Key/value cache operators: views that the kernels take by value, the 4-bit record's offsets, the batch's
+// token -> (request, position) map, and the launchers.  Formats and contracts: include/ivfpq.h.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace ivfpq {
+namespace kv {
+
+constexpr int kTile = 16;                // tokens of a record
+constexpr int kFlagPage = 1;             // a block table entry outside the cache was skipped
+constexpr int kFlagLength = 2;           // a request is longer than its row of the block table
+constexpr int kFlagStart = 4;            // q_start decreases or leaves 0 .. ntok
+constexpr int kFlagWait = 8;             // a bounded wait ran out
+
+// Workspace: [0] status word, then the zeroed words of kv_attend.cu, then partial results.
+constexpr size_t kZeroBytes = IVFPQ_KV_WORKSPACE_ZERO;
+
+struct Cache {
+    int32_t format, d, nheads, page;
+    int32_t page_shift;
+    int64_t npages;
+    char* k;                  // 16-bit formats
+    char* v;
+    int64_t ks[3], vs[3];     // page, head, token strides in elements
+    uint8_t* rec;             // 4-bit records
+    int8_t* bounds;
+    float* scale;
+};
+
+struct Batch {
+    int32_t nreq, max_blocks;
+    int64_t table_stride;
+    const int32_t* table;
+    const int32_t* len;
+    const int32_t* start;     // null: token r is request r's only one
+    int32_t ntok;
+};
+
+struct Rows {                 // a [ntok][heads][d] array of 16-bit values
+    const char* p;
+    int64_t ts, hs;           // token and head strides in elements
+};
+
+// Last request whose first token is at or before `tok` (binary search; start[] has nreq + 1 entries).
+__device__ __forceinline__ int request_of(const Batch& b, int tok) {
+    if (!b.start) return tok;
+    int lo = 0, hi = b.nreq - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (b.start[mid] <= tok) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+// New tokens of request r as [first, first + n), clamped to the batch.
+__device__ __forceinline__ int2 tokens_of(const Batch& b, int r, int* status) {
+    if (!b.start) return make_int2(r, 1);
+    int f = b.start[r], e = b.start[r + 1];
+    if (f < 0 || e < f || e > b.ntok) {
+        if (status) atomicOr(status, kFlagStart);
+        f = min(max(f, 0), b.ntok);
+        e = min(max(e, f), b.ntok);
+    }
+    return make_int2(f, e - f);
+}
+
+// Tokens held by request r, never more than its table row has pages for.
+__device__ __forceinline__ int length_of(const Batch& b, const Cache& c, int r, int* status) {
+    const int64_t cap = (int64_t)b.max_blocks << c.page_shift;
+    const int n = b.len[r];
+    if (n > cap) {
+        if (status) atomicOr(status, kFlagLength);
+        return (int)cap;
+    }
+    return n;
+}
+
+// Physical page of block `blk` of request r, or -1.
+__device__ __forceinline__ int page_of(const Batch& b, const Cache& c, int r, int blk, int* status) {
+    const int p = b.table[(int64_t)r * b.table_stride + blk];
+    if (p < 0 || p >= c.npages) {
+        if (status) atomicOr(status, kFlagPage);
+        return -1;
+    }
+    return p;
+}
+
+__device__ __forceinline__ uint8_t* record_of(const Cache& c, int64_t page, int head, int tile) {
+    return c.rec + ((page * c.nheads + head) * (c.page / kTile) + tile) * (18 * (int64_t)c.d);
+}
+
+// Offsets within a record of 8 consecutive elements (e a multiple of 8) of token t: one 32-bit word.
+__device__ __forceinline__ int key_word(int d, int t, int e) {
+    const int D = min(d, 128), p = e / D, o = e % D;
+    return (p * 16 * D + t * D) / 2 + (o % 64 / 16) * (D / 8) + (o / 64) * 8 + (o % 16) / 2;
+}
+__device__ __forceinline__ int value_word(int d, int t, int e) {
+    const int D = min(d, 128), p = e / D, o = e % D, w = D / 8;
+    return 8 * d + p * 8 * D + (t / 8) * 4 * D + (o / w) * 4 * w + (t % 8) * (w / 2) + (o % w) / 2;
+}
+// Scale and offset of group g of token t (values: the offset is 4 bytes behind the scale).
+__device__ __forceinline__ int key_param(int d, int t, int g) { return 16 * d + (t * (d / 64) + g) * 4; }
+__device__ __forceinline__ int value_param(int d, int t, int g) {
+    return 17 * d + ((t / 8) * (d / 64) + g) * 32 + (t % 8) / 2 * 8 + (t % 2) * 2;
+}
+
+__device__ __forceinline__ float to_float(uint16_t bits, bool bf16) {
+    return bf16 ? __uint_as_float((uint32_t)bits << 16) : __half2float(__ushort_as_half(bits));
+}
+__device__ __forceinline__ uint16_t to_bits(float x, bool bf16) {
+    return bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __half_as_ushort(__float2half_rn(x));
+}
+__device__ __forceinline__ void unpack8(const uint4& w, bool bf16, float* x) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = to_float((uint16_t)(u[i] & 0xffff), bf16);
+        x[2 * i + 1] = to_float((uint16_t)(u[i] >> 16), bf16);
+    }
+}
+__device__ __forceinline__ uint4 pack8(const float* x, bool bf16) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = (uint32_t)to_bits(x[2 * i], bf16) | (uint32_t)to_bits(x[2 * i + 1], bf16) << 16;
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+// What 8 codes of a word stand for (s * u exact in fp32: one rounding).
+__device__ __forceinline__ void decode8(uint32_t w, float s, float z, float* x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __fmaf_rn(s, (float)((w >> (4 * i)) & 15u), z);
+}
+
+// 8-bit codes of values of magnitude <= top: rint(x * (127 * (1 / top))), each step rounded to fp32.
+__device__ __forceinline__ float code_factor(float top) { return top >= 1.17549435e-38f ? __fmul_rn(__frcp_rn(top), 127.f) : 0.f; }
+__device__ __forceinline__ int8_t code8(float x, float factor) {
+    const float y = __fmul_rn(x, factor);          // infinity times 0: code 0
+    return y == y ? (int8_t)__float2int_rn(fminf(fmaxf(y, -127.f), 127.f)) : (int8_t)0;
+}
+
+// Launchers.
+cudaError_t launch_append(const Cache& c, const Batch& b, bool bf16, const Rows& k, const Rows& v, int* status, cudaStream_t st);
+cudaError_t launch_read(const Cache& c, const Batch& b, bool bf16, char* k, char* v, int* status, cudaStream_t st);
+cudaError_t launch_read_bounds(const Cache& c, const int32_t* pages, int64_t n, float* upper, float* lower, int* status, cudaStream_t st);
+struct SelectArgs {
+    Cache c;
+    Batch b;
+    Rows q;
+    bool bf16;
+    int32_t group, nselect, nsink, nlocal;
+    int32_t* out;
+    int* status;
+};
+cudaError_t launch_select(const SelectArgs& a, cudaStream_t st);
+struct AttendArgs {
+    Cache c;
+    Batch b;
+    Rows q;
+    bool bf16;
+    int32_t group, nselect;   // nselect 0: the whole cache
+    float scale;
+    const int32_t* blocks;
+    char* out;
+    float* lse;
+    char* ws;
+};
+cudaError_t launch_attend(const AttendArgs& a, cudaStream_t st);
+size_t attend_workspace_bytes(int d);
+
+}  // namespace kv
+}  // namespace ivfpq

@@ -1,0 +1,207 @@
+// C ABI of the key/value cache operators: argument validation and dispatch.  Contracts: include/ivfpq.h.
+#include <math.h>
+
+#include "kv.cuh"
+
+using namespace ivfpq;
+using namespace ivfpq::kv;
+
+namespace {
+
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+int check_cache(const ivfpq_kv_cache_t* c, Cache* out) {
+    if (!c) return IVFPQ_ERR_INVALID_ARGUMENT;
+    if (c->nheads <= 0 || c->npages <= 0) return IVFPQ_ERR_INVALID_ARGUMENT;
+    if (c->format < IVFPQ_KV_INT4 || c->format > IVFPQ_KV_FP16) return IVFPQ_ERR_UNSUPPORTED;
+    if (c->d != 64 && c->d != 128 && c->d != 256) return IVFPQ_ERR_UNSUPPORTED;
+    if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return IVFPQ_ERR_UNSUPPORTED;
+    if (c->nheads > 1024 || c->npages > 0x7FFFFFFFll) return IVFPQ_ERR_UNSUPPORTED;
+    *out = Cache{};
+    out->format = c->format;
+    out->d = c->d;
+    out->nheads = c->nheads;
+    out->page = c->page;
+    out->page_shift = c->page == 16 ? 4 : c->page == 32 ? 5 : c->page == 64 ? 6 : 7;
+    out->npages = c->npages;
+    if (c->format == IVFPQ_KV_INT4) {
+        if (!c->records || !aligned(c->records, 16)) return IVFPQ_ERR_INVALID_ARGUMENT;
+        out->rec = static_cast<uint8_t*>(c->records);
+    } else {
+        if (!c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16)) return IVFPQ_ERR_INVALID_ARGUMENT;
+        out->k = static_cast<char*>(c->k);
+        out->v = static_cast<char*>(c->v);
+        for (int i = 0; i < 3; ++i) {
+            if (c->k_stride[i] % 8 || c->v_stride[i] % 8) return IVFPQ_ERR_INVALID_ARGUMENT;
+            out->ks[i] = c->k_stride[i];
+            out->vs[i] = c->v_stride[i];
+        }
+    }
+    if ((c->bounds == nullptr) != (c->bounds_scale == nullptr)) return IVFPQ_ERR_INVALID_ARGUMENT;
+    if (!aligned(c->bounds, 16) || !aligned(c->bounds_scale, 4)) return IVFPQ_ERR_INVALID_ARGUMENT;
+    out->bounds = c->bounds;
+    out->scale = c->bounds_scale;
+    return IVFPQ_OK;
+}
+
+int check_batch(const ivfpq_kv_batch_t* b, int64_t ntok, Batch* out) {
+    if (!b || !b->block_table || !b->seq_len) return IVFPQ_ERR_INVALID_ARGUMENT;
+    if (b->nreq <= 0 || b->max_blocks <= 0 || ntok <= 0) return IVFPQ_ERR_INVALID_ARGUMENT;
+    if (b->nreq > 1 && b->table_stride < b->max_blocks) return IVFPQ_ERR_INVALID_ARGUMENT;
+    if (!b->q_start && ntok != b->nreq) return IVFPQ_ERR_INVALID_ARGUMENT;
+    if (b->nreq > 1 << 20 || ntok > 1 << 20 || b->max_blocks > 1 << 24) return IVFPQ_ERR_UNSUPPORTED;
+    if (!aligned(b->block_table, 4) || !aligned(b->seq_len, 4) || !aligned(b->q_start, 4)) return IVFPQ_ERR_INVALID_ARGUMENT;
+    out->nreq = b->nreq;
+    out->max_blocks = b->max_blocks;
+    out->table_stride = b->table_stride;
+    out->table = b->block_table;
+    out->len = b->seq_len;
+    out->start = b->q_start;
+    out->ntok = (int32_t)ntok;
+    return IVFPQ_OK;
+}
+
+int check_dtype(const Cache& c, int32_t dtype) {
+    if (dtype != IVFPQ_KV_BF16 && dtype != IVFPQ_KV_FP16) return IVFPQ_ERR_UNSUPPORTED;
+    if (c.format != IVFPQ_KV_INT4 && dtype != c.format) return IVFPQ_ERR_UNSUPPORTED;
+    return IVFPQ_OK;
+}
+
+int check_rows(const void* p, int64_t ts, int64_t hs) {
+    return p && aligned(p, 16) && ts % 8 == 0 && hs % 8 == 0 ? IVFPQ_OK : IVFPQ_ERR_INVALID_ARGUMENT;
+}
+
+int check_workspace(const Cache& c, const void* ws, size_t bytes) {
+    if (!ws) return IVFPQ_ERR_INVALID_ARGUMENT;
+    return aligned(ws, 256) && bytes >= ivfpq_kv_workspace_bytes(c.d) ? IVFPQ_OK : IVFPQ_ERR_WORKSPACE;
+}
+
+int check_heads(const Cache& c, int32_t nq_heads) {
+    if (nq_heads <= 0 || nq_heads % c.nheads) return IVFPQ_ERR_INVALID_ARGUMENT;
+    return nq_heads / c.nheads > IVFPQ_KV_MAX_GROUP ? IVFPQ_ERR_UNSUPPORTED : IVFPQ_OK;
+}
+
+int done(cudaError_t e) { return e == cudaSuccess ? IVFPQ_OK : IVFPQ_ERR_CUDA; }
+
+}  // namespace
+
+extern "C" {
+
+size_t ivfpq_kv_workspace_bytes(int32_t d) {
+    if (d != 64 && d != 128 && d != 256) return 0;
+    return kZeroBytes + align_up(attend_workspace_bytes(d), 256);
+}
+
+int ivfpq_kv_append(const ivfpq_kv_cache_t* cache, const ivfpq_kv_batch_t* batch, int64_t ntok, int32_t dtype,
+                    const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
+                    int64_t v_token_stride, int64_t v_head_stride, void* workspace, size_t workspace_bytes,
+                    void* stream) {
+    Cache c;
+    Batch b;
+    int rc = check_cache(cache, &c);
+    if (rc == IVFPQ_OK) rc = check_batch(batch, ntok, &b);
+    if (rc == IVFPQ_OK) rc = check_dtype(c, dtype);
+    if (rc == IVFPQ_OK) rc = check_rows(k, k_token_stride, k_head_stride);
+    if (rc == IVFPQ_OK) rc = check_rows(v, v_token_stride, v_head_stride);
+    if (rc == IVFPQ_OK) rc = check_workspace(c, workspace, workspace_bytes);
+    if (rc != IVFPQ_OK) return rc;
+    return done(launch_append(c, b, dtype == IVFPQ_KV_BF16, {static_cast<const char*>(k), k_token_stride, k_head_stride},
+                              {static_cast<const char*>(v), v_token_stride, v_head_stride}, static_cast<int*>(workspace),
+                              static_cast<cudaStream_t>(stream)));
+}
+
+int ivfpq_kv_read(const ivfpq_kv_cache_t* cache, const ivfpq_kv_batch_t* batch, int64_t ntok, int32_t dtype,
+                  void* k_out, void* v_out, void* workspace, size_t workspace_bytes, void* stream) {
+    Cache c;
+    Batch b;
+    int rc = check_cache(cache, &c);
+    if (rc == IVFPQ_OK) rc = check_batch(batch, ntok, &b);
+    if (rc == IVFPQ_OK) rc = check_dtype(c, dtype);
+    if (rc == IVFPQ_OK && (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16))) rc = IVFPQ_ERR_INVALID_ARGUMENT;
+    if (rc == IVFPQ_OK) rc = check_workspace(c, workspace, workspace_bytes);
+    if (rc != IVFPQ_OK) return rc;
+    return done(launch_read(c, b, dtype == IVFPQ_KV_BF16, static_cast<char*>(k_out), static_cast<char*>(v_out),
+                            static_cast<int*>(workspace), static_cast<cudaStream_t>(stream)));
+}
+
+int ivfpq_kv_read_bounds(const ivfpq_kv_cache_t* cache, const int32_t* pages, int64_t n, float* upper, float* lower,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+    Cache c;
+    int rc = check_cache(cache, &c);
+    if (rc != IVFPQ_OK) return rc;
+    if (!c.bounds || !pages || n <= 0 || !upper || !lower || !aligned(pages, 4) || !aligned(upper, 16) || !aligned(lower, 16))
+        return IVFPQ_ERR_INVALID_ARGUMENT;
+    if (n > 1 << 24) return IVFPQ_ERR_UNSUPPORTED;
+    rc = check_workspace(c, workspace, workspace_bytes);
+    if (rc != IVFPQ_OK) return rc;
+    return done(launch_read_bounds(c, pages, n, upper, lower, static_cast<int*>(workspace), static_cast<cudaStream_t>(stream)));
+}
+
+int ivfpq_kv_select(const ivfpq_kv_cache_t* cache, const ivfpq_kv_batch_t* batch, int64_t ntok, int32_t dtype,
+                    const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t nq_heads, int32_t nselect,
+                    int32_t nsink, int32_t nlocal, int32_t* blocks_out, void* workspace, size_t workspace_bytes,
+                    void* stream) {
+    SelectArgs a{};
+    int rc = check_cache(cache, &a.c);
+    if (rc == IVFPQ_OK) rc = check_batch(batch, ntok, &a.b);
+    if (rc == IVFPQ_OK) rc = check_dtype(a.c, dtype);
+    if (rc == IVFPQ_OK) rc = check_rows(q, q_token_stride, q_head_stride);
+    if (rc == IVFPQ_OK) rc = check_heads(a.c, nq_heads);
+    if (rc != IVFPQ_OK) return rc;
+    if (!a.c.bounds || !blocks_out || !aligned(blocks_out, 4)) return IVFPQ_ERR_INVALID_ARGUMENT;
+    if (nsink < 0 || nlocal < 1 || nselect < 1 || (int64_t)nsink + nlocal > nselect) return IVFPQ_ERR_INVALID_ARGUMENT;
+    if (nselect > IVFPQ_KV_MAX_SELECT || a.b.max_blocks > IVFPQ_KV_MAX_BLOCKS) return IVFPQ_ERR_UNSUPPORTED;
+    rc = check_workspace(a.c, workspace, workspace_bytes);
+    if (rc != IVFPQ_OK) return rc;
+    a.q = {static_cast<const char*>(q), q_token_stride, q_head_stride};
+    a.bf16 = dtype == IVFPQ_KV_BF16;
+    a.group = nq_heads / a.c.nheads;
+    a.nselect = nselect;
+    a.nsink = nsink;
+    a.nlocal = nlocal;
+    a.out = blocks_out;
+    a.status = static_cast<int*>(workspace);
+    return done(launch_select(a, static_cast<cudaStream_t>(stream)));
+}
+
+int ivfpq_kv_attend(const ivfpq_kv_cache_t* cache, const ivfpq_kv_batch_t* batch, int64_t ntok, int32_t dtype,
+                    const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t nq_heads, float scale,
+                    const int32_t* blocks, int32_t nselect, void* out, float* lse, void* workspace,
+                    size_t workspace_bytes, void* stream) {
+    AttendArgs a{};
+    int rc = check_cache(cache, &a.c);
+    if (rc == IVFPQ_OK) rc = check_batch(batch, ntok, &a.b);
+    if (rc == IVFPQ_OK) rc = check_dtype(a.c, dtype);
+    if (rc == IVFPQ_OK) rc = check_rows(q, q_token_stride, q_head_stride);
+    if (rc == IVFPQ_OK) rc = check_heads(a.c, nq_heads);
+    if (rc != IVFPQ_OK) return rc;
+    if (!out || !aligned(out, 16) || !aligned(lse, 4) || !aligned(blocks, 4)) return IVFPQ_ERR_INVALID_ARGUMENT;
+    if (!isfinite(scale)) return IVFPQ_ERR_INVALID_ARGUMENT;
+    if (blocks ? nselect < 1 : nselect != 0) return IVFPQ_ERR_INVALID_ARGUMENT;
+    if (nselect > IVFPQ_KV_MAX_SELECT) return IVFPQ_ERR_UNSUPPORTED;
+    rc = check_workspace(a.c, workspace, workspace_bytes);
+    if (rc != IVFPQ_OK) return rc;
+    a.q = {static_cast<const char*>(q), q_token_stride, q_head_stride};
+    a.bf16 = dtype == IVFPQ_KV_BF16;
+    a.group = nq_heads / a.c.nheads;
+    a.nselect = nselect;
+    a.scale = scale;
+    a.blocks = blocks;
+    a.out = static_cast<char*>(out);
+    a.lse = lse;
+    a.ws = static_cast<char*>(workspace);
+    return done(launch_attend(a, static_cast<cudaStream_t>(stream)));
+}
+
+int ivfpq_kv_status(void* workspace, void* stream) {
+    if (!workspace) return IVFPQ_ERR_INVALID_ARGUMENT;
+    if (!aligned(workspace, 256)) return IVFPQ_ERR_WORKSPACE;
+    int flags = 0;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (cudaMemcpyAsync(&flags, workspace, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess) return IVFPQ_ERR_CUDA;
+    if (cudaMemsetAsync(workspace, 0, 4, st) != cudaSuccess) return IVFPQ_ERR_CUDA;
+    if (cudaStreamSynchronize(st) != cudaSuccess) return IVFPQ_ERR_CUDA;
+    return flags ? IVFPQ_ERR_DEVICE_FLAG : IVFPQ_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,244 @@
+// Writing tokens to the paged cache, and reading it back.  Formats: include/ivfpq.h.
+#include "kv.cuh"
+
+namespace ivfpq {
+namespace kv {
+namespace {
+
+constexpr int kThreads = 128;
+
+// One CTA writes the new tokens of one (request, block, kv head).  A token's d elements are spread over d / 8
+// lanes, 8 consecutive elements (16 bytes in, one 32-bit word of codes out) each, so that a group of 64 is 8
+// neighbouring lanes and its extrema are three shuffles.  When the block becomes full its bounds follow from the held
+// values: those of the tokens just written come from registers, older ones are read back from the cache.
+//
+// Work items: request r owns items base(r) .. base(r + 1) - 1 with base(r) = start[r] / page + 2 r, at least as many as
+// the blocks its new tokens can lie in; the item's request is found by binary search, surplus items end at once.
+template <int D>
+__global__ void __launch_bounds__(kThreads) append_kernel(Cache c, Batch b, bool bf16, Rows k, Rows v, int* status) {
+    constexpr int kLanes = D / 8;                 // lanes per token
+    constexpr int kRows = kThreads / kLanes;      // tokens per pass
+    __shared__ float s_hi[kRows][D], s_lo[kRows][D];
+    __shared__ float s_top[kThreads / 32];
+    const int head = blockIdx.y, item = blockIdx.x;
+    int r = item, blk0 = 0;
+    if (b.start) {
+        int lo = 0, hi = b.nreq - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if ((b.start[mid] >> c.page_shift) + 2 * mid <= item) lo = mid; else hi = mid - 1;
+        }
+        r = lo;
+        blk0 = item - ((b.start[r] >> c.page_shift) + 2 * r);
+        if (blk0 < 0) return;
+    }
+    const int2 tok = tokens_of(b, r, status);
+    const int len = length_of(b, c, r, status);
+    const int first = max(len - tok.y, 0);        // first new position that is written
+    if (tok.y <= 0 || len <= first) return;
+    const int blk = (first >> c.page_shift) + blk0;
+    const int p0 = blk << c.page_shift;           // first position of the block
+    if (p0 >= len) return;
+    const int page = page_of(b, c, r, blk, status);
+    if (page < 0) return;
+    const bool full = c.bounds && p0 + c.page <= len;
+    const int lane = threadIdx.x % kLanes, row = threadIdx.x / kLanes, e = lane * 8;
+    const int t_begin = full ? 0 : max(first - p0, 0), t_end = min(c.page, len - p0);
+    float hi[8], lo[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        hi[i] = -INFINITY;
+        lo[i] = INFINITY;
+    }
+    for (int t0 = t_begin; t0 < t_end; t0 += kRows) {
+        const int t = t0 + row;
+        if (t >= t_end) continue;                 // whole groups of kLanes lanes
+        const bool fresh = p0 + t >= first;
+        const int64_t src = tok.x + (p0 + t - (len - tok.y));
+        float x[8];
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+            if (kv == 1 && !fresh) break;
+            if (c.format != IVFPQ_KV_INT4) {
+                char* at = kv ? c.v + 2 * (page * c.vs[0] + head * c.vs[1] + t * c.vs[2] + e)
+                              : c.k + 2 * (page * c.ks[0] + head * c.ks[1] + t * c.ks[2] + e);
+                uint4 w;
+                if (fresh) {
+                    const Rows& in = kv ? v : k;
+                    w = *reinterpret_cast<const uint4*>(in.p + 2 * (src * in.ts + head * in.hs + e));
+                    *reinterpret_cast<uint4*>(at) = w;
+                } else {
+                    w = *reinterpret_cast<const uint4*>(at);
+                }
+                if (!kv) unpack8(w, c.format == IVFPQ_KV_BF16, x);
+            } else {
+                uint8_t* rec = record_of(c, page, head, t / kTile);
+                const int tt = t % kTile, g = e / 64;
+                uint32_t* wp = reinterpret_cast<uint32_t*>(rec + (kv ? value_word(D, tt, e) : key_word(D, tt, e)));
+                __half* sp = reinterpret_cast<__half*>(rec + (kv ? value_param(D, tt, g) : key_param(D, tt, g)));
+                __half* zp = sp + (kv ? 2 : 1);
+                if (fresh) {
+                    const Rows& in = kv ? v : k;
+                    float y[8];
+                    unpack8(*reinterpret_cast<const uint4*>(in.p + 2 * (src * in.ts + head * in.hs + e)), bf16, y);
+                    float mn = INFINITY, mx = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        y[i] = fminf(fmaxf(y[i], -65504.f), 65504.f);
+                        mn = fminf(mn, y[i]);
+                        mx = fmaxf(mx, y[i]);
+                    }
+                    const unsigned m = 0xffu << (threadIdx.x % 32 / 8 * 8);
+#pragma unroll
+                    for (int o = 4; o; o >>= 1) {
+                        mn = fminf(mn, __shfl_xor_sync(m, mn, o));
+                        mx = fmaxf(mx, __shfl_xor_sync(m, mx, o));
+                    }
+                    const __half hz = __float2half_rn(mn);
+                    const float z = __half2float(hz);
+                    const __half hs = __float2half_rn(__fmul_rn(__fsub_rn(mx, z), 1.f / 15.f));
+                    const float s = __half2float(hs);
+                    uint32_t w = 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float u = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(y[i], z), s)), 0.f), 15.f) : 0.f;
+                        w |= (uint32_t)u << (4 * i);
+                    }
+                    *wp = w;
+                    if (lane % 8 == 0) {
+                        *sp = hs;
+                        *zp = hz;
+                    }
+                    if (!kv) decode8(w, s, z, x);
+                } else {
+                    decode8(*wp, __half2float(*sp), __half2float(*zp), x);
+                }
+            }
+            if (!kv) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    hi[i] = fmaxf(hi[i], x[i]);
+                    lo[i] = fminf(lo[i], x[i]);
+                }
+            }
+        }
+    }
+    if (!full) return;                            // uniform over the CTA
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        s_hi[row][e + i] = hi[i];
+        s_lo[row][e + i] = lo[i];
+    }
+    __syncthreads();
+    float top = 0.f;
+    for (int i = threadIdx.x; i < D; i += kThreads) {
+        float a = s_hi[0][i], z = s_lo[0][i];
+        for (int j = 1; j < kRows; ++j) {
+            a = fmaxf(a, s_hi[j][i]);
+            z = fminf(z, s_lo[j][i]);
+        }
+        s_hi[0][i] = a;
+        s_lo[0][i] = z;
+        top = fmaxf(top, fmaxf(fabsf(a), fabsf(z)));
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (threadIdx.x % 32 == 0) s_top[threadIdx.x / 32] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+    const float inv = code_factor(top);
+    int8_t* out = c.bounds + ((int64_t)page * c.nheads + head) * 2 * D;
+    for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
+        const float x = i < D ? s_hi[0][i] : s_lo[0][i - D];
+        out[i] = code8(x, inv);
+    }
+    if (threadIdx.x == 0) c.scale[(int64_t)page * c.nheads + head] = __fmul_rn(top, 1.f / 127.f);
+}
+
+// 8 elements of one (token, head) per thread.
+__global__ void __launch_bounds__(256) read_kernel(Cache c, Batch b, bool bf16, char* k, char* v, int* status) {
+    const int per_head = c.d / 8, per_tok = c.nheads * per_head;
+    const int64_t total = (int64_t)b.ntok * per_tok;
+    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= total) return;
+    const int tok = (int)(i / per_tok), rest = (int)(i - (int64_t)tok * per_tok), head = rest / per_head, e = rest % per_head * 8;
+    const int r = request_of(b, tok);
+    const int2 mine = tokens_of(b, r, status);
+    const int len = length_of(b, c, r, status);
+    const int pos = len - mine.y + (tok - mine.x);
+    uint4 wk = make_uint4(0, 0, 0, 0), wv = wk;
+    if (pos >= 0 && pos < len) {
+        const int page = page_of(b, c, r, pos >> c.page_shift, status);
+        const int t = pos & (c.page - 1);
+        if (page >= 0) {
+            if (c.format != IVFPQ_KV_INT4) {
+                wk = *reinterpret_cast<const uint4*>(c.k + 2 * (page * c.ks[0] + head * c.ks[1] + t * c.ks[2] + e));
+                wv = *reinterpret_cast<const uint4*>(c.v + 2 * (page * c.vs[0] + head * c.vs[1] + t * c.vs[2] + e));
+            } else {
+                const uint8_t* rec = record_of(c, page, head, t / kTile);
+                const int tt = t % kTile, g = e / 64;
+                const __half* kp = reinterpret_cast<const __half*>(rec + key_param(c.d, tt, g));
+                const __half* vp = reinterpret_cast<const __half*>(rec + value_param(c.d, tt, g));
+                float x[8];
+                decode8(*reinterpret_cast<const uint32_t*>(rec + key_word(c.d, tt, e)), __half2float(kp[0]), __half2float(kp[1]), x);
+                wk = pack8(x, bf16);
+                decode8(*reinterpret_cast<const uint32_t*>(rec + value_word(c.d, tt, e)), __half2float(vp[0]), __half2float(vp[2]), x);
+                wv = pack8(x, bf16);
+            }
+        }
+    }
+    reinterpret_cast<uint4*>(k)[i] = wk;
+    reinterpret_cast<uint4*>(v)[i] = wv;
+}
+
+// 4 channels of one (page, head) per thread.
+__global__ void __launch_bounds__(256) read_bounds_kernel(Cache c, const int32_t* pages, int64_t n, float4* upper, float4* lower,
+                                                          int* status) {
+    const int per_head = c.d / 4, per_page = c.nheads * per_head;
+    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= n * per_page) return;
+    const int64_t j = i / per_page;
+    const int rest = (int)(i - j * per_page), head = rest / per_head, e = rest % per_head * 4;
+    const int page = pages[j];
+    float4 hi = make_float4(0.f, 0.f, 0.f, 0.f), lo = hi;
+    if (page < 0 || page >= c.npages) {
+        atomicOr(status, kFlagPage);
+    } else {
+        const int64_t at = (int64_t)page * c.nheads + head;
+        const float s = c.scale[at];
+        const char4 a = *reinterpret_cast<const char4*>(c.bounds + at * 2 * c.d + e);
+        const char4 z = *reinterpret_cast<const char4*>(c.bounds + at * 2 * c.d + c.d + e);
+        hi = make_float4(__fmul_rn(a.x, s), __fmul_rn(a.y, s), __fmul_rn(a.z, s), __fmul_rn(a.w, s));
+        lo = make_float4(__fmul_rn(z.x, s), __fmul_rn(z.y, s), __fmul_rn(z.z, s), __fmul_rn(z.w, s));
+    }
+    upper[i] = hi;
+    lower[i] = lo;
+}
+
+}  // namespace
+
+cudaError_t launch_append(const Cache& c, const Batch& b, bool bf16, const Rows& k, const Rows& v, int* status, cudaStream_t st) {
+    const int items = b.start ? (b.ntok >> c.page_shift) + 2 * b.nreq : b.nreq;
+    const dim3 grid(items, c.nheads);
+    if (c.d == 64) append_kernel<64><<<grid, kThreads, 0, st>>>(c, b, bf16, k, v, status);
+    else if (c.d == 128) append_kernel<128><<<grid, kThreads, 0, st>>>(c, b, bf16, k, v, status);
+    else append_kernel<256><<<grid, kThreads, 0, st>>>(c, b, bf16, k, v, status);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_read(const Cache& c, const Batch& b, bool bf16, char* k, char* v, int* status, cudaStream_t st) {
+    const int64_t total = (int64_t)b.ntok * c.nheads * (c.d / 8);
+    read_kernel<<<(unsigned)((total + 255) / 256), 256, 0, st>>>(c, b, bf16, k, v, status);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_read_bounds(const Cache& c, const int32_t* pages, int64_t n, float* upper, float* lower, int* status, cudaStream_t st) {
+    const int64_t total = n * c.nheads * (c.d / 4);
+    if ((total + 255) / 256 > 0x7FFFFFFFll) return cudaErrorInvalidValue;
+    read_bounds_kernel<<<(unsigned)((total + 255) / 256), 256, 0, st>>>(c, pages, n, reinterpret_cast<float4*>(upper),
+                                                                         reinterpret_cast<float4*>(lower), status);
+    return cudaGetLastError();
+}
+
+}  // namespace kv
+}  // namespace ivfpq

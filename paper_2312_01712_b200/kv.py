@@ -1,0 +1,247 @@
+"""ctypes binding of the key/value cache entry points of `include/ivfpq.h` (`ivfpq_kv_*`): a paged
+cache in 4 or 16 bits, block filtering by the bounds of the keys, attention over the whole cache or over the
+chosen blocks.  Argument marshalling only, as in `binding.py`."""
+
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import Optional, Tuple
+
+import torch
+
+from . import binding
+from .binding import IVFPQ_ERR_UNSUPPORTED, IvfpqError, _check
+
+IVFPQ_KV_INT4 = 0
+IVFPQ_KV_BF16 = 1
+IVFPQ_KV_FP16 = 2
+IVFPQ_KV_MAX_SELECT = 1024
+IVFPQ_KV_MAX_GROUP = 64
+IVFPQ_KV_MAX_BLOCKS = 32768
+IVFPQ_KV_WORKSPACE_ZERO = 8192
+
+_FORMAT = {torch.bfloat16: IVFPQ_KV_BF16, torch.float16: IVFPQ_KV_FP16}
+_HELD = {IVFPQ_KV_BF16: torch.bfloat16, IVFPQ_KV_FP16: torch.float16}
+
+
+class ivfpq_kv_cache_t(ctypes.Structure):
+    _fields_ = [("format", ctypes.c_int32), ("d", ctypes.c_int32), ("nheads", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("npages", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3), ("records", ctypes.c_void_p),
+                ("bounds", ctypes.c_void_p), ("bounds_scale", ctypes.c_void_p)]
+
+
+class ivfpq_kv_batch_t(ctypes.Structure):
+    _fields_ = [("nreq", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("table_stride", ctypes.c_int64),
+                ("block_table", ctypes.c_void_p), ("seq_len", ctypes.c_void_p), ("q_start", ctypes.c_void_p)]
+
+
+_lib: Optional[ctypes.CDLL] = None
+
+
+def _load() -> ctypes.CDLL:
+    global _lib
+    if _lib is None:
+        lib = binding.load_library()
+        vp, i32, i64, sz, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
+        lib.ivfpq_kv_workspace_bytes.argtypes = [i32]
+        lib.ivfpq_kv_workspace_bytes.restype = sz
+        lib.ivfpq_kv_append.argtypes = [vp, vp, i64, i32, vp, i64, i64, vp, i64, i64, vp, sz, vp]
+        lib.ivfpq_kv_read.argtypes = [vp, vp, i64, i32, vp, vp, vp, sz, vp]
+        lib.ivfpq_kv_read_bounds.argtypes = [vp, vp, i64, vp, vp, vp, sz, vp]
+        lib.ivfpq_kv_select.argtypes = [vp, vp, i64, i32, vp, i64, i64, i32, i32, i32, i32, vp, vp, sz, vp]
+        lib.ivfpq_kv_attend.argtypes = [vp, vp, i64, i32, vp, i64, i64, i32, f32, vp, i32, vp, vp, vp, sz, vp]
+        lib.ivfpq_kv_status.argtypes = [vp, vp]
+        for f in (lib.ivfpq_kv_append, lib.ivfpq_kv_read, lib.ivfpq_kv_read_bounds, lib.ivfpq_kv_select, lib.ivfpq_kv_attend,
+                  lib.ivfpq_kv_status):
+            f.restype = ctypes.c_int
+        _lib = lib
+    return _lib
+
+
+def ivfpq_kv_workspace_bytes(d: int) -> int:
+    return int(_load().ivfpq_kv_workspace_bytes(d))
+
+
+class KvCacheHandle:
+    """A paged key/value cache on tensors of the caller's: `records` uint8 [pages, heads, page / 16, 18 * d]
+    (4 bits) or `k` and `v` [pages, heads, page, d] (bf16 or fp16, any strides with the last axis contiguous);
+    `bounds` int8 [pages, heads, 2, d] and `bounds_scale` fp32 [pages, heads] if blocks are to be selected.
+    One workspace per stream that calls are made on belongs to the handle."""
+
+    def __init__(self, records: Optional[torch.Tensor] = None, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+                 bounds: Optional[torch.Tensor] = None, bounds_scale: Optional[torch.Tensor] = None):
+        if (records is None) == (k is None) or (k is None) != (v is None):
+            raise ValueError("a cache is either records or k and v")
+        s = ivfpq_kv_cache_t()
+        if records is not None:
+            if records.dtype != torch.uint8 or not records.is_cuda or not records.is_contiguous() or records.dim() != 4 \
+                    or records.shape[3] % 18:
+                raise ValueError("records must be a contiguous uint8 CUDA tensor [pages, heads, page / 16, 18 * d]")
+            s.format, s.d, s.page = IVFPQ_KV_INT4, records.shape[3] // 18, records.shape[2] * 16
+            s.records, first = records.data_ptr(), records
+        else:
+            for x in (k, v):
+                if x.dtype not in _FORMAT or not x.is_cuda or x.dim() != 4 or x.stride(3) != 1 or x.shape != k.shape or x.dtype != k.dtype:
+                    raise ValueError("k and v must be bf16 or fp16 CUDA tensors [pages, heads, page, d], contiguous in d")
+            s.format, s.d, s.page = _FORMAT[k.dtype], k.shape[3], k.shape[2]
+            s.k, s.v, first = k.data_ptr(), v.data_ptr(), k
+            s.k_stride[:], s.v_stride[:] = k.stride()[:3], v.stride()[:3]
+        s.npages, s.nheads = first.shape[0], first.shape[1]
+        if (bounds is None) != (bounds_scale is None):
+            raise ValueError("bounds and bounds_scale belong together")
+        if bounds is not None:
+            if bounds.dtype != torch.int8 or not bounds.is_contiguous() or tuple(bounds.shape) != (s.npages, s.nheads, 2, s.d) \
+                    or bounds_scale.dtype != torch.float32 or not bounds_scale.is_contiguous() \
+                    or tuple(bounds_scale.shape) != (s.npages, s.nheads) or bounds.device != first.device \
+                    or bounds_scale.device != first.device:
+                raise ValueError("bounds must be int8 [pages, heads, 2, d] and bounds_scale fp32 [pages, heads], contiguous, on the cache's device")
+            s.bounds, s.bounds_scale = bounds.data_ptr(), bounds_scale.data_ptr()
+        self.struct, self.format, self.d, self.page, self.npages, self.nheads = s, s.format, s.d, s.page, s.npages, s.nheads
+        self.device, self.dtype = first.device, _HELD.get(s.format)
+        self.records, self.k, self.v, self.bounds, self.bounds_scale = records, k, v, bounds, bounds_scale
+        self._ref = ctypes.addressof(s)
+        self._nbytes = ivfpq_kv_workspace_bytes(s.d)
+        if self._nbytes == 0 or s.page not in (16, 32, 64, 128):
+            raise IvfpqError(IVFPQ_ERR_UNSUPPORTED, "KvCacheHandle")
+        self._ws: dict = {}
+
+    @classmethod
+    def empty(cls, npages: int, nheads: int, page: int, d: int, dtype=None, bounds: bool = True, device="cuda") -> "KvCacheHandle":
+        """A zeroed cache: 4 bits (`dtype` None), bf16 or fp16."""
+        b = dict(bounds=torch.zeros(npages, nheads, 2, d, dtype=torch.int8, device=device),
+                 bounds_scale=torch.zeros(npages, nheads, dtype=torch.float32, device=device)) if bounds else {}
+        if dtype is None:
+            return cls(records=torch.zeros(npages, nheads, page // 16, 18 * d, dtype=torch.uint8, device=device), **b)
+        return cls(k=torch.zeros(npages, nheads, page, d, dtype=dtype, device=device),
+                   v=torch.zeros(npages, nheads, page, d, dtype=dtype, device=device), **b)
+
+    def workspace(self, stream: int) -> torch.Tensor:
+        """The workspace of calls on `stream`: calls on two streams may overlap, so each has its own."""
+        ws = self._ws.get(stream)
+        if ws is None:
+            ws = torch.empty(self._nbytes, dtype=torch.uint8, device=self.device)
+            ws[:IVFPQ_KV_WORKSPACE_ZERO].zero_()
+            self._ws[stream] = ws
+        return ws
+
+    def _call(self) -> Tuple[int, int]:
+        stream = torch.cuda.current_stream(self.device).cuda_stream
+        ws = self._ws.get(stream)
+        return stream, (self.workspace(stream) if ws is None else ws).data_ptr()
+
+
+class KvBatchHandle:
+    """Requests of one step: `block_table` int32 [requests, blocks], `seq_len` int32 [requests] (tokens held, the
+    step's included), `q_start` int32 [requests + 1] or None (one token per request); device tensors, read by the
+    kernels when they run."""
+
+    def __init__(self, block_table: torch.Tensor, seq_len: torch.Tensor, q_start: Optional[torch.Tensor] = None):
+        n = seq_len.shape[0]
+        for x, shape in ((block_table, (n, block_table.shape[-1])), (seq_len, (n,)), (q_start, (n + 1,))):
+            if x is not None and (x.dtype != torch.int32 or not x.is_cuda or tuple(x.shape) != shape or x.stride(-1) != 1):
+                raise ValueError("block_table [n, blocks], seq_len [n] and q_start [n + 1] must be int32 CUDA tensors")
+        self.block_table, self.seq_len, self.q_start = block_table, seq_len, q_start
+        self.struct = ivfpq_kv_batch_t(n, block_table.shape[1], block_table.stride(0), block_table.data_ptr(), seq_len.data_ptr(),
+                                       None if q_start is None else q_start.data_ptr())
+        self._ref = ctypes.addressof(self.struct)
+
+
+def _rows(x: torch.Tensor, cache: KvCacheHandle, what: str) -> int:
+    if x.dtype not in _FORMAT or x.dim() != 3 or x.shape[2] != cache.d or x.stride(2) != 1 or x.device != cache.device:
+        raise ValueError(f"{what} must be a bf16 or fp16 tensor [tokens, heads, {cache.d}] on the cache's device, contiguous in the last axis")
+    return _FORMAT[x.dtype]
+
+
+def ivfpq_kv_append(cache: KvCacheHandle, batch: KvBatchHandle, k: torch.Tensor, v: torch.Tensor) -> None:
+    """Writes the step's keys and values [tokens, heads, d] to the cache."""
+    dt = _rows(k, cache, "k")
+    if _rows(v, cache, "v") != dt or k.shape != v.shape or k.shape[1] != cache.nheads:
+        raise ValueError("k and v must be of one type and [tokens, kv heads, d]")
+    stream, ws = cache._call()
+    ks, vs = k.stride(), v.stride()
+    _check(_load().ivfpq_kv_append(cache._ref, batch._ref, k.shape[0], dt, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
+                                   ws, cache._nbytes, stream), "ivfpq_kv_append")
+
+
+def ivfpq_kv_read(cache: KvCacheHandle, batch: KvBatchHandle, ntok: int, dtype: Optional[torch.dtype] = None,
+                  out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
+    """The held keys and values of the step's `ntok` tokens, each [tokens, heads, d]."""
+    if out is None:
+        dtype = dtype or cache.dtype or torch.bfloat16
+        out = tuple(torch.empty((ntok, cache.nheads, cache.d), dtype=dtype, device=cache.device) for _ in range(2))
+    k, v = out
+    if k.shape[0] != ntok:
+        raise ValueError("out must have ntok rows")
+    dt = _rows(k, cache, "out[0]")
+    if _rows(v, cache, "out[1]") != dt or k.shape != v.shape or k.shape[1] != cache.nheads or not k.is_contiguous() or not v.is_contiguous():
+        raise ValueError("out must be two contiguous tensors [tokens, kv heads, d] of one type")
+    stream, ws = cache._call()
+    _check(_load().ivfpq_kv_read(cache._ref, batch._ref, k.shape[0], dt, k.data_ptr(), v.data_ptr(), ws, cache._nbytes, stream),
+           "ivfpq_kv_read")
+    return k, v
+
+
+def ivfpq_kv_read_bounds(cache: KvCacheHandle, pages: torch.Tensor):
+    """Upper and lower bounds of the keys of physical `pages` (int32 [n]), each fp32 [n, heads, d]."""
+    if pages.dtype != torch.int32 or pages.dim() != 1 or not pages.is_contiguous() or pages.device != cache.device:
+        raise ValueError("pages must be a contiguous int32 tensor on the cache's device")
+    hi = torch.empty((pages.shape[0], cache.nheads, cache.d), dtype=torch.float32, device=cache.device)
+    lo = torch.empty_like(hi)
+    stream, ws = cache._call()
+    _check(_load().ivfpq_kv_read_bounds(cache._ref, pages.data_ptr(), pages.shape[0], hi.data_ptr(), lo.data_ptr(), ws, cache._nbytes,
+                                        stream), "ivfpq_kv_read_bounds")
+    return hi, lo
+
+
+def ivfpq_kv_select(cache: KvCacheHandle, batch: KvBatchHandle, q: torch.Tensor, nselect: int, nsink: int = 1, nlocal: int = 1,
+                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Blocks to attend over, int32 [tokens, kv heads, nselect], ascending, padded with -1, for queries
+    [tokens, query heads, d]."""
+    dt = _rows(q, cache, "q")
+    if out is None:
+        out = torch.empty((q.shape[0], cache.nheads, nselect), dtype=torch.int32, device=q.device)
+    elif out.dtype != torch.int32 or tuple(out.shape) != (q.shape[0], cache.nheads, nselect) or not out.is_contiguous() \
+            or out.device != cache.device:
+        raise ValueError("out must be a contiguous int32 tensor [tokens, kv heads, nselect] on the cache's device")
+    stream, ws = cache._call()
+    qs = q.stride()
+    _check(_load().ivfpq_kv_select(cache._ref, batch._ref, q.shape[0], dt, q.data_ptr(), qs[0], qs[1], q.shape[1], nselect, nsink,
+                                   nlocal, out.data_ptr(), ws, cache._nbytes, stream), "ivfpq_kv_select")
+    return out
+
+
+def ivfpq_kv_attend(cache: KvCacheHandle, batch: KvBatchHandle, q: torch.Tensor, blocks: Optional[torch.Tensor] = None,
+                    scale: Optional[float] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of q [tokens, query heads, d] over the cache up to each token's position, whole or over `blocks`
+    (as ivfpq_kv_select lists them); `scale` defaults to 1 / sqrt(d).  Returns out; `lse` fp32 [tokens, query heads]
+    is filled if given."""
+    dt = _rows(q, cache, "q")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif out.dtype != q.dtype or out.shape != q.shape or not out.is_contiguous() or out.device != cache.device:
+        raise ValueError("out must be a contiguous tensor like q")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.device != cache.device):
+        raise ValueError("lse must be a contiguous fp32 tensor [tokens, query heads]")
+    nselect = 0
+    if blocks is not None:
+        if blocks.dtype != torch.int32 or blocks.dim() != 3 or blocks.shape[0] != q.shape[0] or blocks.shape[1] != cache.nheads \
+                or not blocks.is_contiguous() or blocks.device != cache.device:
+            raise ValueError("blocks must be a contiguous int32 tensor [tokens, kv heads, nselect]")
+        nselect = blocks.shape[2]
+    stream, ws = cache._call()
+    qs = q.stride()
+    _check(_load().ivfpq_kv_attend(cache._ref, batch._ref, q.shape[0], dt, q.data_ptr(), qs[0], qs[1], q.shape[1],
+                                   1.0 / math.sqrt(cache.d) if scale is None else scale, None if blocks is None else blocks.data_ptr(),
+                                   nselect, out.data_ptr(), None if lse is None else lse.data_ptr(), ws, cache._nbytes, stream),
+           "ivfpq_kv_attend")
+    return out
+
+
+def ivfpq_kv_status(cache: KvCacheHandle) -> int:
+    """Synchronises the current stream and returns (and clears) the device status of the calls made on it."""
+    stream = torch.cuda.current_stream(cache.device).cuda_stream
+    if stream not in cache._ws:
+        return binding.IVFPQ_OK
+    return int(_load().ivfpq_kv_status(cache._ws[stream].data_ptr(), stream))
