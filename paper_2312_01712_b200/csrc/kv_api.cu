@@ -44,12 +44,12 @@ int check_cache(const ivfpq_kv_cache_t* c, Cache* out) {
     return IVFPQ_OK;
 }
 
-int check_batch(const ivfpq_kv_batch_t* b, int64_t ntok, Batch* out) {
+int check_batch(const ivfpq_kv_batch_t* b, const Cache& c, int64_t ntok, Batch* out) {
     if (!b || !b->block_table || !b->seq_len) return IVFPQ_ERR_INVALID_ARGUMENT;
     if (b->nreq <= 0 || b->max_blocks <= 0 || ntok <= 0) return IVFPQ_ERR_INVALID_ARGUMENT;
     if (b->nreq > 1 && b->table_stride < b->max_blocks) return IVFPQ_ERR_INVALID_ARGUMENT;
     if (!b->q_start && ntok != b->nreq) return IVFPQ_ERR_INVALID_ARGUMENT;
-    if (b->nreq > 1 << 20 || ntok > 1 << 20 || b->max_blocks > 1 << 24) return IVFPQ_ERR_UNSUPPORTED;
+    if (b->nreq > 1 << 20 || ntok > 1 << 20 || (int64_t)b->max_blocks * c.page > 1 << 30) return IVFPQ_ERR_UNSUPPORTED;
     if (!aligned(b->block_table, 4) || !aligned(b->seq_len, 4) || !aligned(b->q_start, 4)) return IVFPQ_ERR_INVALID_ARGUMENT;
     out->nreq = b->nreq;
     out->max_blocks = b->max_blocks;
@@ -99,7 +99,7 @@ int ivfpq_kv_append(const ivfpq_kv_cache_t* cache, const ivfpq_kv_batch_t* batch
     Cache c;
     Batch b;
     int rc = check_cache(cache, &c);
-    if (rc == IVFPQ_OK) rc = check_batch(batch, ntok, &b);
+    if (rc == IVFPQ_OK) rc = check_batch(batch, c, ntok, &b);
     if (rc == IVFPQ_OK) rc = check_dtype(c, dtype);
     if (rc == IVFPQ_OK) rc = check_rows(k, k_token_stride, k_head_stride);
     if (rc == IVFPQ_OK) rc = check_rows(v, v_token_stride, v_head_stride);
@@ -115,7 +115,7 @@ int ivfpq_kv_read(const ivfpq_kv_cache_t* cache, const ivfpq_kv_batch_t* batch, 
     Cache c;
     Batch b;
     int rc = check_cache(cache, &c);
-    if (rc == IVFPQ_OK) rc = check_batch(batch, ntok, &b);
+    if (rc == IVFPQ_OK) rc = check_batch(batch, c, ntok, &b);
     if (rc == IVFPQ_OK) rc = check_dtype(c, dtype);
     if (rc == IVFPQ_OK && (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16))) rc = IVFPQ_ERR_INVALID_ARGUMENT;
     if (rc == IVFPQ_OK) rc = check_workspace(c, workspace, workspace_bytes);
@@ -143,7 +143,7 @@ int ivfpq_kv_select(const ivfpq_kv_cache_t* cache, const ivfpq_kv_batch_t* batch
                     void* stream) {
     SelectArgs a{};
     int rc = check_cache(cache, &a.c);
-    if (rc == IVFPQ_OK) rc = check_batch(batch, ntok, &a.b);
+    if (rc == IVFPQ_OK) rc = check_batch(batch, a.c, ntok, &a.b);
     if (rc == IVFPQ_OK) rc = check_dtype(a.c, dtype);
     if (rc == IVFPQ_OK) rc = check_rows(q, q_token_stride, q_head_stride);
     if (rc == IVFPQ_OK) rc = check_heads(a.c, nq_heads);
@@ -170,7 +170,7 @@ int ivfpq_kv_attend(const ivfpq_kv_cache_t* cache, const ivfpq_kv_batch_t* batch
                     size_t workspace_bytes, void* stream) {
     AttendArgs a{};
     int rc = check_cache(cache, &a.c);
-    if (rc == IVFPQ_OK) rc = check_batch(batch, ntok, &a.b);
+    if (rc == IVFPQ_OK) rc = check_batch(batch, a.c, ntok, &a.b);
     if (rc == IVFPQ_OK) rc = check_dtype(a.c, dtype);
     if (rc == IVFPQ_OK) rc = check_rows(q, q_token_stride, q_head_stride);
     if (rc == IVFPQ_OK) rc = check_heads(a.c, nq_heads);

@@ -1,93 +1,852 @@
 // Attention over the paged key/value cache, whole or over listed blocks.
+//
+// For a kv head, the rows of a tile are up to 8 NT (token, query head) pairs that share it.  Transposed products keep those few
+// rows on the short side of the matrix instruction:
+//   S^T [16 keys x 8 rows] = K Q^T,   O^T [d x 8 rows] += V^T P^T   (mma m16n8k16, fp32 accumulators),
+// so one kv head with 8 query heads fills it.  A decode step reads every key and value once for a handful of
+// rows, which leaves it bound by memory; what the kernel is built for is bytes in flight and few instructions per byte:
+//   - each warp owns a ring of stages in shared memory (16 or 32 keys each) and waits for nobody else;
+//   - 4-bit records arrive by bulk copies on an mbarrier, 16-bit rows by cp.async into a swizzled tile;
+//   - 4-bit key codes enter the product as they are: (w & 0x000f000f) read as two fp16 numbers is u * 2^-24, (w & 0x00f000f0) is
+//     16 u * 2^-24, exact subnormals, and the group's scale and offset are applied to the fp32 sums:
+//       q.k = sum over groups of s * sum(u q) + z * sum(q);
+//     five logic instructions unpack 8 codes.  Value codes are scaled in fp16 (u s + z, one rounding), since their scale runs
+//     along the summed axis;
+//   - the running maximum moves only when a logit exceeds it by more than 2^8 (in the exponent of 2), which bounds p by
+//     256 and saves the shuffles and the rescaling of O in almost every stage.
+//
+// The keys of all (tile, kv head) pairs form one line of units of 128 keys, cut into equal parts, one per CTA, so that
+// ragged lengths load all SMs alike.  A pair that is cut leaves fp32 partial results in the workspace; the CTA
+// that finishes last (a ticket per pair) adds them in a fixed order: results do not depend on timing.
+#include <type_traits>
+
 #include "kv.cuh"
 
 namespace ivfpq {
 namespace kv {
 namespace {
 
-// One warp per (token, query head): a lane holds d / 32 consecutive elements, one key at a time, running maximum
-// and sum of the softmax (online form: a larger maximum m' scales what was summed by exp(m - m')).
-template <int E>
-__global__ void __launch_bounds__(128) attend_kernel(AttendArgs a) {
-    const Cache& c = a.c;
-    const int lane = threadIdx.x % 32, e = lane * E, hq = a.group * c.nheads;
-    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
-    if (row >= (int64_t)a.b.ntok * hq) return;
-    const int tok = (int)(row / hq), h = (int)(row % hq), head = h / a.group;
-    int* status = reinterpret_cast<int*>(a.ws);
-    const int r = request_of(a.b, tok);
-    const int2 mine = tokens_of(a.b, r, status);
-    const int len = length_of(a.b, c, r, status);
-    const int pos = len - mine.y + (tok - mine.x);
-    const int nb = pos < 0 || pos >= len ? 0 : (pos >> c.page_shift) + 1;
-    float q[E], o[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-        q[i] = to_float(reinterpret_cast<const uint16_t*>(a.q.p + 2 * (tok * a.q.ts + h * a.q.hs))[e + i], a.bf16) * a.scale;
-        o[i] = 0.f;
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kUnit = 128;               // keys of a unit: 32 per warp
+constexpr int kMaxCtas = 640;            // CTAs that share work (tickets and partial results in the workspace)
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.f;
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <bool BF>
+__device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if (BF)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ void ldmatrix4(uint32_t* r, uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4t(uint32_t* r, uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+template <bool BF>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t y;
+    if (BF) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+    return y;
+}
+__device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t y;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(a), "r"(b), "r"(c));
+    return y;
+}
+__device__ __forceinline__ uint32_t hadd2(uint32_t a, uint32_t b) {
+    uint32_t y;
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+    return y;
+}
+// Copies 16 bytes, or zeros where !real.
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool real) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(n) : "memory"); }
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok;
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+// Shape of an instance.
+template <int FMT, int D, int NT>
+struct Shape {
+    static constexpr bool kInt4 = FMT == IVFPQ_KV_INT4;
+    static constexpr int kRows = 8 * NT;
+    static constexpr int kStageKeys = kInt4 ? 32 : 16;
+    static constexpr int kSubs = kStageKeys / 16;
+    static constexpr int kStageBytes = kInt4 ? kSubs * 18 * D : 16 * D * 2 * 2;
+    static constexpr int kStages = kInt4 ? 4 : (D == 64 ? 4 : 3);
+    static constexpr int kRingBytes = kStages * kStageBytes;
+    static constexpr int kSmem = kWarps * kRingBytes;
+    static constexpr int kMinCtas = D == 256 ? 1 : (kInt4 && NT == 1 ? 3 : 2);
+    static_assert(kRingBytes >= kRows * (D + 4) * 4, "a warp's ring holds its O");
+};
+
+struct Plan {
+    int32_t ntiles;          // row tiles (an upper bound where requests have several tokens)
+    int32_t per_token;       // tiles of a request with one token, or of a listed token
+    int32_t whole;           // 1: one CTA per (tile, kv head), nothing is cut
+};
+
+// Rows of a tile: request, its first row (of n_tokens * group), and how many keys its last row sees.
+struct Tile {
+    int r, row0, nrows, tok0, len, n;   // nrows: rows of the request in all
+    __device__ int limit(int row, int group) const { return max(len - n + row / group + 1, 0); }
+};
+
+template <int R, bool LIST>
+__device__ __forceinline__ bool tile_of(const AttendArgs& a, const Plan& p, int t, Tile* out, int* status) {
+    const Batch& b = a.b;
+    int r, i;
+    if (LIST) {
+        // tiles are of single tokens: token t / per_token
+        const int tok = t / p.per_token;
+        r = request_of(b, tok);
+        const int2 tk = tokens_of(b, r, status);
+        const int j = tok - tk.x;
+        if (j < 0 || j >= tk.y) return false;
+        const int len = length_of(b, a.c, r, status);
+        *out = {r, (t % p.per_token) * R, a.group, tok, len - tk.y + j + 1, 1};
+        return true;
     }
-    float m = -INFINITY, l = 0.f;
-    const int32_t* list = a.blocks ? a.blocks + ((int64_t)tok * c.nheads + head) * a.nselect : nullptr;
-    const int n = list ? a.nselect : nb;
-    for (int j = 0; j < n; ++j) {
-        const int blk = list ? list[j] : j;
-        if (blk < 0 || blk >= nb) continue;
-        const int page = page_of(a.b, c, r, blk, status);
-        if (page < 0) continue;
-        const int end = min(c.page, pos + 1 - (blk << c.page_shift));
-        for (int t = 0; t < end; ++t) {
-            float kx[E], vx[E];
-            if (c.format != IVFPQ_KV_INT4) {
-                const uint16_t* kp = reinterpret_cast<const uint16_t*>(c.k) + page * c.ks[0] + head * c.ks[1] + t * c.ks[2] + e;
-                const uint16_t* vp = reinterpret_cast<const uint16_t*>(c.v) + page * c.vs[0] + head * c.vs[1] + t * c.vs[2] + e;
+    if (!b.start) {
+        r = t / p.per_token;
+        i = t % p.per_token;
+    } else {
+        int lo = 0, hi = b.nreq - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if ((int64_t)b.start[mid] * a.group / R + mid <= t) lo = mid; else hi = mid - 1;
+        }
+        r = lo;
+        const int64_t base = (int64_t)b.start[r] * a.group / R + r;
+        if (t < base) return false;
+        i = (int)(t - base);
+    }
+    const int2 tk = tokens_of(b, r, status);
+    if ((int64_t)i * R >= (int64_t)tk.y * a.group) return false;
+    *out = {r, i * R, tk.y * a.group, tk.x, length_of(b, a.c, r, status), tk.y};
+    return true;
+}
+
+template <int FMT, int D, int NT, bool LIST>
+__global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) attend_kernel(AttendArgs a, Plan plan) {
+    using S = Shape<FMT, D, NT>;
+    constexpr bool kInt4 = S::kInt4;
+    constexpr bool BF = FMT == IVFPQ_KV_BF16;
+    constexpr int R = S::kRows, G = D / 64, KSTEPS = D / 16, MT = D / 16;
+    extern __shared__ __align__(128) char smem[];
+    __shared__ __align__(8) uint64_t s_bar[kWarps][S::kStages];
+    __shared__ int s_info[kWarps][S::kStages][2];
+    __shared__ float s_ml[kWarps][R][2];
+    __shared__ long long s_scan[kWarps + 1];
+    __shared__ int s_start[3];
+    __shared__ int s_last;
+
+    const Cache& c = a.c;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, lr = lane / 4, lc = lane % 4;
+    int* status = reinterpret_cast<int*>(a.ws);
+    int* tickets = reinterpret_cast<int*>(a.ws + 256);
+    float* part_o = reinterpret_cast<float*>(a.ws + kZeroBytes);
+    float* part_ml = part_o + (size_t)2 * kMaxCtas * R * D;
+    char* ring = smem + warp * S::kRingBytes;
+    const uint32_t ring_u = smem_u32(ring);
+
+    if (kInt4 && lane == 0) {
+        for (int i = 0; i < S::kStages; ++i) mbar_init(smem_u32(&s_bar[warp][i]), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    uint32_t phase = 0;                       // parity bit of every stage of the warp's ring
+    bool dead = false;                        // a bounded wait ran out
+
+    auto units_of = [&](int t, Tile* tl) -> int {
+        if (!tile_of<R, LIST>(a, plan, t, tl, status)) return 0;
+        if (LIST) return max(1, (a.nselect * c.page + kUnit - 1) / kUnit);
+        const int last = min(tl->row0 + R, tl->nrows) - 1;
+        return max(1, (tl->limit(last, a.group) + kUnit - 1) / kUnit);
+    };
+
+    // ---- the CTA's part of the line of units ----
+    long long total = 0, first = 0, end = 0, tile_base = 0;   // tile_base: first unit of tile `t`
+    long long ctas = 1;                                       // that have a part: none is empty
+    int t = 0;
+    Tile tl{};
+    int units = 0;
+    if (plan.whole) {
+        t = blockIdx.x;
+        units = units_of(t, &tl);
+        if (units == 0) return;
+        first = (long long)blockIdx.y * units;
+        end = first + units;
+    } else {
+        const int per = (plan.ntiles + kThreads - 1) / kThreads;
+        const int t_lo = min(tid * per, plan.ntiles), t_hi = min(t_lo + per, plan.ntiles);
+        long long sum = 0;
+        for (int i = t_lo; i < t_hi; ++i) {
+            Tile x;
+            sum += units_of(i, &x);
+        }
+        sum *= c.nheads;
+        long long inc = sum;
 #pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    kx[i] = to_float(kp[i], a.bf16);
-                    vx[i] = to_float(vp[i], a.bf16);
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += y;
+        }
+        if (lane == 31) s_scan[warp] = inc;
+        __syncthreads();
+        long long base = inc - sum;
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) base += s_scan[w];
+            total += s_scan[w];
+        }
+        ctas = min((long long)gridDim.x, total);
+        if (blockIdx.x >= ctas) return;
+        first = total * blockIdx.x / ctas;
+        end = total * (blockIdx.x + 1) / ctas;
+        if (base <= first && first < base + sum) {
+            for (int i = t_lo; i < t_hi; ++i) {
+                Tile x;
+                const long long n = (long long)units_of(i, &x) * c.nheads;
+                if (first < base + n) {
+                    s_start[0] = i;
+                    s_scan[kWarps] = base;
+                    break;
                 }
-            } else {
-                const uint8_t* rec = record_of(c, page, head, t / kTile);
-                const int tt = t % kTile, g = e / 64, e8 = e / 8 * 8, sh = e % 8 * 4;
-                const __half* kp = reinterpret_cast<const __half*>(rec + key_param(c.d, tt, g));
-                const __half* vp = reinterpret_cast<const __half*>(rec + value_param(c.d, tt, g));
-                const uint32_t kw = *reinterpret_cast<const uint32_t*>(rec + key_word(c.d, tt, e8)) >> sh;
-                const uint32_t vw = *reinterpret_cast<const uint32_t*>(rec + value_word(c.d, tt, e8)) >> sh;
+                base += n;
+            }
+        }
+        __syncthreads();
+        t = s_start[0];
+        tile_base = s_scan[kWarps];
+        units = units_of(t, &tl);
+    }
+
+    for (long long at = first; at < end;) {
+        while (at >= tile_base + (long long)units * c.nheads) {      // next tile with work
+            tile_base += (long long)units * c.nheads;
+            ++t;
+            units = units_of(t, &tl);
+        }
+        const int head = (int)((at - tile_base) / units);
+        const int u0 = (int)(at - tile_base - (long long)head * units);
+        const int u1 = (int)min((long long)units, u0 + (end - at));
+        const int rows = min(R, tl.nrows - tl.row0);
+        const int lim_lo = tl.limit(tl.row0, a.group), lim_hi = tl.limit(tl.row0 + rows - 1, a.group);
+        const int vlen = LIST ? a.nselect << c.page_shift : lim_hi;
+        const int32_t* list = LIST ? a.blocks + ((int64_t)tl.tok0 * c.nheads + head) * a.nselect : nullptr;
+
+        // ---- 16-key pieces of the warp: piece s covers (virtual) keys (u0 + s / 2) 128 + 32 warp + 16 (s % 2) ----
+        const int nsub = (u1 - u0) * 2, nstage = nsub / S::kSubs;
+        int pg_cur = -1, pos_cur = 0, pg_nxt = -1, pos_nxt = 0;
+        auto look = [&](int s, int* pg, int* pos) {
+            *pg = -1;
+            *pos = 0;
+            if (s >= nsub) return;
+            const int vk = (u0 + (s >> 1)) * kUnit + warp * 32 + (s & 1) * 16;
+            if (vk >= vlen) return;
+            int blk = vk >> c.page_shift;
+            if (LIST) {
+                blk = list[blk];
+                if (blk < 0 || (int64_t)blk << c.page_shift >= lim_hi) return;
+            }
+            *pos = (blk << c.page_shift) + (vk & (c.page - 1));
+            if (*pos >= lim_hi) return;
+            *pg = page_of(a.b, c, tl.r, blk, status);
+        };
+        look(lane, &pg_cur, &pos_cur);
+        look(lane + 32, &pg_nxt, &pos_nxt);
+        auto issue = [&](int st) {            // stage st of the segment into its slot
+            if (st < nstage) {
+                const int slot = st % S::kStages;
+                const int s0 = st * S::kSubs;
+                if (s0 && s0 % 32 == 0) {
+                    pg_cur = pg_nxt;
+                    pos_cur = pos_nxt;
+                    look(s0 + 32 + lane, &pg_nxt, &pos_nxt);
+                }
+                int pg[S::kSubs], pos[S::kSubs];
 #pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    kx[i] = fmaf(__half2float(kp[0]), (float)((kw >> (4 * i)) & 15u), __half2float(kp[1]));
-                    vx[i] = fmaf(__half2float(vp[0]), (float)((vw >> (4 * i)) & 15u), __half2float(vp[2]));
+                for (int i = 0; i < S::kSubs; ++i) {
+                    pg[i] = __shfl_sync(0xffffffffu, pg_cur, (s0 + i) & 31);
+                    pos[i] = __shfl_sync(0xffffffffu, pos_cur, (s0 + i) & 31);
+                }
+                if (kInt4) {
+                    if (lane == 0) {
+                        uint32_t bytes = 0;
+#pragma unroll
+                        for (int i = 0; i < S::kSubs; ++i) {
+                            s_info[warp][slot][i] = pg[i] >= 0 && !dead ? pos[i] : -1;
+                            if (pg[i] >= 0) bytes += 18 * D;
+                        }
+                        if (bytes && !dead) {
+                            const uint32_t bar = smem_u32(&s_bar[warp][slot]);
+                            mbar_expect(bar, bytes);
+#pragma unroll
+                            for (int i = 0; i < S::kSubs; ++i)
+                                if (pg[i] >= 0)
+                                    bulk_load(ring_u + slot * S::kStageBytes + i * 18 * D,
+                                              record_of(c, pg[i], head, (pos[i] & (c.page - 1)) >> 4), 18 * D, bar);
+                        }
+                    }
+                } else {
+                    if (lane == 0) s_info[warp][slot][0] = pg[0] >= 0 ? pos[0] : -1;
+                    if (pg[0] >= 0) {
+                        constexpr int CH = D / 8;                         // 16-byte chunks of a row
+                        const int tk = pos[0] & (c.page - 1);
+                        const char* kp = c.k + 2 * (pg[0] * c.ks[0] + head * c.ks[1] + tk * c.ks[2]);
+                        const char* vp = c.v + 2 * (pg[0] * c.vs[0] + head * c.vs[1] + tk * c.vs[2]);
+                        const uint32_t dst = ring_u + slot * S::kStageBytes;
+#pragma unroll
+                        for (int i = 0; i < 16 * CH / 32; ++i) {
+                            const int x = i * 32 + lane, row = x / CH, ch = x % CH;
+                            const uint32_t o = row * (2 * D) + ((ch ^ (row & 7)) * 16);
+                            const bool real = pos[0] + row < lim_hi;
+                            const int rr = real ? row : 0;
+                            cp_async16(dst + o, kp + 2 * (rr * c.ks[2] + ch * 8), real);
+                            cp_async16(dst + 16 * D * 2 + o, vp + 2 * (rr * c.vs[2] + ch * 8), real);
+                        }
+                    }
                 }
             }
-            float x = 0.f;
+            if (!kInt4) cp_async_commit();
+        };
+
+        // the ring was used for the previous segment's O: order those accesses before the copies
+        if (kInt4) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
 #pragma unroll
-            for (int i = 0; i < E; ++i) x = fmaf(q[i], kx[i], x);
+        for (int i = 0; i < S::kStages - 1; ++i) issue(i);
+
+        // ---- queries ----
+        uint32_t qf[NT][KSTEPS][2];
+        float qs[NT][kInt4 ? G : 1][2];       // 4-bit: sums of a column's query elements over each group, times 2^-24
+        float cf[NT][2];                      // factor from products to base-2 logits
+        int lim[NT][2];
 #pragma unroll
-            for (int s = 16; s; s >>= 1) x += __shfl_xor_sync(0xffffffffu, x, s);
-            const float mn = fmaxf(m, x), f = __expf(m - mn), p = __expf(x - mn);
-            m = mn;
-            l = l * f + p;
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = tl.row0 + nt * 8 + lr;
+            const bool real = row < tl.nrows;
+            const int j = real ? row / a.group : 0, g = real ? row % a.group : 0;
+            const char* qp = a.q.p + 2 * ((int64_t)(tl.tok0 + j) * a.q.ts + (int64_t)(head * a.group + g) * a.q.hs);
+            if (!kInt4) {
 #pragma unroll
-            for (int i = 0; i < E; ++i) o[i] = fmaf(p, vx[i], o[i] * f);
+                for (int s = 0; s < KSTEPS; ++s) {
+                    qf[nt][s][0] = real ? *reinterpret_cast<const uint32_t*>(qp + 2 * (16 * s + 2 * lc)) : 0u;
+                    qf[nt][s][1] = real ? *reinterpret_cast<const uint32_t*>(qp + 2 * (16 * s + 8 + 2 * lc)) : 0u;
+                }
+                cf[nt][0] = cf[nt][1] = a.scale * kLog2e;
+            } else {
+                // the lane's words (group, half): elements 64 group + 16 lc + 8 half + 0..7, scaled by a power of two to just below 2^15
+                uint4 raw[G][2];
+                float top = 0.f;
+#pragma unroll
+                for (int gr = 0; gr < G; ++gr)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        raw[gr][h] = real ? *reinterpret_cast<const uint4*>(qp + 2 * (64 * gr + 16 * lc + 8 * h)) : make_uint4(0, 0, 0, 0);
+                        float x[8];
+                        unpack8(raw[gr][h], a.bf16, x);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+                    }
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const int ex = top > 0.f ? min(max(14 - ((int)(__float_as_uint(top) >> 23) - 127), -100), 100) : 0;
+                const float up = __uint_as_float((uint32_t)(127 + ex) << 23);
+                const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
+#pragma unroll
+                for (int gr = 0; gr < G; ++gr) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float x[8];
+                        unpack8(raw[gr][h], a.bf16, x);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            x[i] *= up;
+                            sum += x[i];
+                        }
+                        const int s = (gr * 2 + h) * 2;
+                        qf[nt][s][0] = pack2<false>(x[0], x[4]);
+                        qf[nt][s][1] = pack2<false>(x[1] * 0.0625f, x[5] * 0.0625f);
+                        qf[nt][s + 1][0] = pack2<false>(x[2], x[6]);
+                        qf[nt][s + 1][1] = pack2<false>(x[3] * 0.0625f, x[7] * 0.0625f);
+                    }
+                    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                    sum *= 5.9604644775390625e-08f;                       // 2^-24
+                    qs[nt][gr][0] = __shfl_sync(0xffffffffu, sum, lc * 8);
+                    qs[nt][gr][1] = __shfl_sync(0xffffffffu, sum, lc * 8 + 4);
+                }
+                const float f = a.scale * kLog2e * 16777216.f * down;     // 2^24
+                cf[nt][0] = __shfl_sync(0xffffffffu, f, lc * 8);
+                cf[nt][1] = __shfl_sync(0xffffffffu, f, lc * 8 + 4);
+            }
+#pragma unroll
+            for (int j2 = 0; j2 < 2; ++j2) {
+                const int col = tl.row0 + nt * 8 + lc * 2 + j2;
+                lim[nt][j2] = col < tl.nrows ? tl.limit(col, a.group) : lim_hi;
+            }
         }
-    }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + row * c.d + e;
+
+        float o[MT][NT][4], m[NT][2], l[NT][2];
 #pragma unroll
-    for (int i = 0; i < E; ++i) out[i] = to_bits(o[i] * inv, a.bf16);
-    if (a.lse && lane == 0) a.lse[row] = l > 0.f ? m + logf(l) : -INFINITY;
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) o[i][nt][x] = 0.f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            m[nt][0] = m[nt][1] = -INFINITY;
+            l[nt][0] = l[nt][1] = 0.f;
+        }
+
+        for (int st = 0; st < nstage; ++st) {
+            const int slot = st % S::kStages;
+            __syncwarp();                     // everybody is done with the slot that is filled next
+            issue(st + S::kStages - 1);
+            if (!kInt4) cp_async_wait<S::kStages - 1>();
+            __syncwarp();
+            int pos[S::kSubs];
+            bool any = false;
+#pragma unroll
+            for (int i = 0; i < S::kSubs; ++i) {
+                pos[i] = s_info[warp][slot][i];
+                any |= pos[i] >= 0;
+            }
+            if (!any) continue;               // uniform over the warp
+            if (kInt4) {
+                const uint32_t bar = smem_u32(&s_bar[warp][slot]);
+                bool ok = false;
+                for (int spin = 0; spin < (1 << 20) && !ok; ++spin) ok = mbar_try(bar, (phase >> slot) & 1);
+                phase ^= 1u << slot;
+                if (!__all_sync(0xffffffffu, ok)) {      // the data never came: no more copies, the flag says so
+                    if (lane == 0) atomicOr(status, kFlagWait);
+                    dead = true;
+                }
+            }
+            const char* buf = ring + slot * S::kStageBytes;
+            const uint32_t buf_u = ring_u + slot * S::kStageBytes;
+            float p[S::kSubs][NT][4];
+
+            // ---- logits ----
+#pragma unroll
+            for (int i = 0; i < S::kSubs; ++i) {
+                if (pos[i] < 0) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) p[i][nt][x] = -INFINITY;
+                    continue;
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) p[i][nt][x] = 0.f;
+                if (kInt4) {
+                    constexpr int GP = D >= 128 ? 2 : 1;                  // groups of a plane
+                    const char* rec = buf + i * 18 * D;
+#pragma unroll
+                    for (int pl = 0; pl < G / GP; ++pl) {
+                        uint32_t w0[GP * 2], w1[GP * 2];
+                        if (GP == 2) {
+                            const uint4 x = *reinterpret_cast<const uint4*>(rec + pl * 1024 + lane * 16);
+                            const uint4 y = *reinterpret_cast<const uint4*>(rec + pl * 1024 + 512 + lane * 16);
+                            w0[0] = x.x; w0[1] = x.y; w0[GP] = x.z; w0[GP + 1] = x.w;
+                            w1[0] = y.x; w1[1] = y.y; w1[GP] = y.z; w1[GP + 1] = y.w;
+                        } else {
+                            const uint2 x = *reinterpret_cast<const uint2*>(rec + lane * 8);
+                            const uint2 y = *reinterpret_cast<const uint2*>(rec + 256 + lane * 8);
+                            w0[0] = x.x; w0[1] = x.y;
+                            w1[0] = y.x; w1[1] = y.y;
+                        }
+#pragma unroll
+                        for (int g = 0; g < GP; ++g) {
+                            const int gr = pl * GP + g;
+                            float acc[NT][4];
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) acc[nt][x] = 0.f;
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const uint32_t x = w0[g * 2 + h], y = w1[g * 2 + h], xs = x >> 8, ys = y >> 8;
+                                const int s = (gr * 2 + h) * 2;
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    mma16816<false>(acc[nt], x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, qf[nt][s][0], qf[nt][s][1]);
+                                    mma16816<false>(acc[nt], xs & 0x000f000fu, ys & 0x000f000fu, xs & 0x00f000f0u, ys & 0x00f000f0u, qf[nt][s + 1][0], qf[nt][s + 1][1]);
+                                }
+                            }
+                            const float2 a0 = __half22float2(*reinterpret_cast<const __half2*>(rec + 16 * D + (lr * G + gr) * 4));
+                            const float2 a1 = __half22float2(*reinterpret_cast<const __half2*>(rec + 16 * D + ((lr + 8) * G + gr) * 4));
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                p[i][nt][0] = fmaf(acc[nt][0], a0.x, fmaf(a0.y, qs[nt][gr][0], p[i][nt][0]));
+                                p[i][nt][1] = fmaf(acc[nt][1], a0.x, fmaf(a0.y, qs[nt][gr][1], p[i][nt][1]));
+                                p[i][nt][2] = fmaf(acc[nt][2], a1.x, fmaf(a1.y, qs[nt][gr][0], p[i][nt][2]));
+                                p[i][nt][3] = fmaf(acc[nt][3], a1.x, fmaf(a1.y, qs[nt][gr][1], p[i][nt][3]));
+                            }
+                        }
+                    }
+                } else {
+                    const int row = (lane & 7) + ((lane >> 3) & 1) * 8, hi = lane >> 4;
+#pragma unroll
+                    for (int s = 0; s < KSTEPS; ++s) {
+                        uint32_t f[4];
+                        ldmatrix4(f, buf_u + row * (2 * D) + (((2 * s + hi) ^ (row & 7)) * 16));
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma16816<BF>(p[i][nt], f[0], f[1], f[2], f[3], qf[nt][s][0], qf[nt][s][1]);
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) p[i][nt][x] *= cf[nt][x & 1];
+                if (pos[i] + 16 > lim_lo) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            if (pos[i] + lr + (x >> 1) * 8 >= lim[nt][x & 1]) p[i][nt][x] = -INFINITY;
+                }
+            }
+
+            // ---- running maximum ----
+            float top[NT][2];
+            bool need = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    float y = fmaxf(p[0][nt][x], p[0][nt][x + 2]);
+                    if (S::kSubs == 2) y = fmaxf(y, fmaxf(p[S::kSubs - 1][nt][x], p[S::kSubs - 1][nt][x + 2]));
+                    top[nt][x] = y;
+                    need |= y > m[nt][x] + kSlack;
+                }
+            if (__any_sync(0xffffffffu, need)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        float y = top[nt][x];
+#pragma unroll
+                        for (int s = 4; s < 32; s <<= 1) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, s));
+                        const float mn = fmaxf(m[nt][x], y);
+                        const float f = m[nt][x] == mn ? 1.f : ex2(m[nt][x] - mn);
+                        m[nt][x] = mn;
+                        l[nt][x] *= f;
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) {
+                            o[i][nt][x] *= f;
+                            o[i][nt][x + 2] *= f;
+                        }
+                    }
+            }
+            uint32_t pf[S::kSubs][NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
+#pragma unroll
+                for (int i = 0; i < S::kSubs; ++i) {
+                    const float e0 = ex2(p[i][nt][0] - m0), e1 = ex2(p[i][nt][1] - m1), e2 = ex2(p[i][nt][2] - m0), e3 = ex2(p[i][nt][3] - m1);
+                    l[nt][0] += e0 + e2;
+                    l[nt][1] += e1 + e3;
+                    pf[i][nt][0] = movmatrix(pack2<BF>(e0, e1));
+                    pf[i][nt][1] = movmatrix(pack2<BF>(e2, e3));
+                }
+            }
+
+            // ---- O^T += V^T P^T ----
+#pragma unroll
+            for (int i = 0; i < S::kSubs; ++i) {
+                if (pos[i] < 0) continue;
+                if (kInt4) {
+                    constexpr int DP = D >= 128 ? 128 : 64, W = DP / 64, GP = DP / 64;
+                    const char* rec = buf + i * 18 * D;
+                    const bool tail = pos[i] + 16 > lim_hi;
+#pragma unroll
+                    for (int pl = 0; pl < D / DP; ++pl) {
+                        const int gr = pl * GP + (GP == 2 ? lr / 4 : 0);      // the lane's 16 (or 8) elements lie in one group
+                        uint32_t sc[2], zr[2], w[2][2][W];                    // [octet][parity][word]
+#pragma unroll
+                        for (int oc = 0; oc < 2; ++oc) {
+                            const uint2 sz = *reinterpret_cast<const uint2*>(rec + 17 * D + ((oc * G + gr) * 4 + lc) * 8);
+                            sc[oc] = sz.x;
+                            zr[oc] = sz.y;
+                            if (tail) {                                       // keys that nobody holds: zeros
+                                const int k0 = pos[i] + oc * 8 + lc * 2;
+                                const uint32_t mask = (k0 < lim_hi ? 0xffffu : 0u) | (k0 + 1 < lim_hi ? 0xffff0000u : 0u);
+                                sc[oc] &= mask;
+                                zr[oc] &= mask;
+                            }
+                            const char* at = rec + 8 * D + pl * 8 * DP + oc * 4 * DP + lane * (8 * W);
+                            if (W == 2) {
+                                const uint4 x = *reinterpret_cast<const uint4*>(at);
+                                w[oc][0][0] = x.x; w[oc][0][W - 1] = x.y;
+                                w[oc][1][0] = x.z; w[oc][1][W - 1] = x.w;
+                            } else {
+                                const uint2 x = *reinterpret_cast<const uint2*>(at);
+                                w[oc][0][0] = x.x;
+                                w[oc][1][0] = x.y;
+                            }
+                        }
+#pragma unroll
+                        for (int wi = 0; wi < W; ++wi)
+#pragma unroll
+                            for (int hf = 0; hf < 2; ++hf) {
+                                uint32_t x[2];
+#pragma unroll
+                                for (int oc = 0; oc < 2; ++oc)
+                                    x[oc] = __byte_perm(w[oc][0][wi], w[oc][1][wi], hf ? 0x7632 : 0x5410);
+#pragma unroll
+                                for (int q = 0; q < 2; ++q) {
+                                    uint32_t f[4];
+#pragma unroll
+                                    for (int oc = 0; oc < 2; ++oc) {
+                                        const uint32_t y = q ? x[oc] >> 8 : x[oc];
+                                        // fp16 1024 + u and 1024 + 16 u: u exactly, then the group's scale and offset
+                                        const uint32_t u0 = hadd2((y & 0x000f000fu) | 0x64006400u, 0xe400e400u);
+                                        const uint32_t u1h = hfma2((y & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, 0xd400d400u);
+                                        f[oc * 2] = hfma2(u0, sc[oc], zr[oc]);
+                                        f[oc * 2 + 1] = hfma2(u1h, sc[oc], zr[oc]);
+                                    }
+                                    const int mt = pl * (DP / 16) + wi * 4 + hf * 2 + q;
+#pragma unroll
+                                    for (int nt = 0; nt < NT; ++nt) mma16816<false>(o[mt][nt], f[0], f[1], f[2], f[3], pf[i][nt][0], pf[i][nt][1]);
+                                }
+                            }
+                    }
+                } else {
+                    const int key = (lane & 7) + (lane >> 4) * 8, hi = (lane >> 3) & 1;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        uint32_t f[4];
+                        ldmatrix4t(f, buf_u + 16 * D * 2 + key * (2 * D) + (((2 * mt + hi) ^ (key & 7)) * 16));
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma16816<BF>(o[mt][nt], f[0], f[1], f[2], f[3], pf[i][nt][0], pf[i][nt][1]);
+                    }
+                }
+            }
+        }
+        if (!kInt4) cp_async_wait<0>();
+
+        // ---- the warps' results side by side: [row][d], rows padded by 4 words ----
+        __syncwarp();
+        float* so = reinterpret_cast<float*>(ring);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                float y = l[nt][x];
+#pragma unroll
+                for (int s = 4; s < 32; s <<= 1) y += __shfl_xor_sync(0xffffffffu, y, s);
+                const int row = nt * 8 + lc * 2 + x;
+                if (lr == 0) {
+                    s_ml[warp][row][0] = m[nt][x];
+                    s_ml[warp][row][1] = y;
+                }
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    const int d0 = !kInt4 ? mt * 16 + lr : D >= 128 ? mt / 8 * 128 + lr * 16 + mt % 8 * 2 : lr * 8 + mt * 2;
+                    so[row * (D + 4) + d0] = o[mt][nt][x];
+                    so[row * (D + 4) + d0 + (kInt4 ? 1 : 8)] = o[mt][nt][x + 2];
+                }
+            }
+        __syncthreads();
+        const bool cut = u0 > 0 || u1 < units;
+        const int slot0 = 2 * blockIdx.x + (at == first ? 0 : 1);
+        auto write_out = [&](int row, int d0, const float* x, float lsum, float mx) {
+            const int rr = tl.row0 + row, j = rr / a.group, g = rr % a.group;
+            const int64_t orow = (int64_t)(tl.tok0 + j) * (c.nheads * a.group) + head * a.group + g;
+            const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+            const bool bf = a.bf16;
+            uint2 w;
+            const bool nan = lsum != lsum;
+            float y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = nan ? lsum : x[i] * inv;
+            w.x = (uint32_t)to_bits(y[0], bf) | (uint32_t)to_bits(y[1], bf) << 16;
+            w.y = (uint32_t)to_bits(y[2], bf) | (uint32_t)to_bits(y[3], bf) << 16;
+            *reinterpret_cast<uint2*>(a.out + 2 * (orow * D + d0)) = w;
+            if (a.lse && d0 == 0) a.lse[orow] = nan ? lsum : lsum > 0.f ? (mx + log2f(lsum)) * 0.6931471805599453f : -INFINITY;
+        };
+        for (int i = tid; i < rows * (D / 4); i += kThreads) {
+            const int row = i / (D / 4), d0 = i % (D / 4) * 4;
+            float mx = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, s_ml[w][row][0]);
+            float x[4] = {0.f, 0.f, 0.f, 0.f}, ls = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float mw = s_ml[w][row][0];
+                const float f = mw == -INFINITY ? 0.f : ex2(mw - mx);
+                const float4 y = *reinterpret_cast<const float4*>(smem + w * S::kRingBytes + (row * (D + 4) + d0) * 4);
+                if (mw != -INFINITY || s_ml[w][row][1] != 0.f) {
+                    x[0] = fmaf(f, y.x, x[0]);
+                    x[1] = fmaf(f, y.y, x[1]);
+                    x[2] = fmaf(f, y.z, x[2]);
+                    x[3] = fmaf(f, y.w, x[3]);
+                    ls = fmaf(f, s_ml[w][row][1], ls);
+                }
+            }
+            if (!cut) {
+                write_out(row, d0, x, ls, mx);
+            } else {
+                const size_t pr = (size_t)slot0 * R + row;
+                *reinterpret_cast<float4*>(part_o + pr * D + d0) = make_float4(x[0], x[1], x[2], x[3]);
+                if (d0 == 0) *reinterpret_cast<float2*>(part_ml + pr * 2) = make_float2(mx, ls);
+            }
+        }
+        if (cut) {
+            // CTAs whose part touches this pair; the last one to arrive adds all in order
+            const long long pa = tile_base + (long long)head * units, pz = pa + units - 1;
+            const int c0 = (int)(((pa + 1) * ctas - 1) / total), c1 = (int)(((pz + 1) * ctas - 1) / total);
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                const int old = atomicAdd(&tickets[c0], 1);
+                s_last = old == c1 - c0;
+                if (s_last) tickets[c0] = 0;
+                __threadfence();
+            }
+            __syncthreads();
+            if (s_last) {
+                for (int i = tid; i < rows * (D / 4); i += kThreads) {
+                    const int row = i / (D / 4), d0 = i % (D / 4) * 4;
+                    float mx = -INFINITY;
+                    for (int k = c0; k <= c1; ++k) {
+                        const int sl = 2 * k + (k == c0 && total * k / ctas != pa ? 1 : 0);
+                        mx = fmaxf(mx, __ldcg(part_ml + ((size_t)sl * R + row) * 2));
+                    }
+                    float x[4] = {0.f, 0.f, 0.f, 0.f}, ls = 0.f;
+#pragma unroll 4
+                    for (int k = c0; k <= c1; ++k) {
+                        const int sl = 2 * k + (k == c0 && total * k / ctas != pa ? 1 : 0);
+                        const size_t pr = (size_t)sl * R + row;
+                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(part_ml + pr * 2));
+                        const float4 y = __ldcg(reinterpret_cast<const float4*>(part_o + pr * D + d0));
+                        const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - mx);
+                        if (ml.x != -INFINITY || ml.y != 0.f) {
+                            x[0] = fmaf(f, y.x, x[0]);
+                            x[1] = fmaf(f, y.y, x[1]);
+                            x[2] = fmaf(f, y.z, x[2]);
+                            x[3] = fmaf(f, y.w, x[3]);
+                            ls = fmaf(f, ml.y, ls);
+                        }
+                    }
+                    write_out(row, d0, x, ls, mx);
+                }
+            }
+        }
+        at += u1 - u0;
+        if (at < end) __syncthreads();        // the rings hold O until here
+    }
+    if (kInt4 && dead) {
+        // copies may still be on their way into this CTA's memory: wait for them, again within a limit
+        for (int i = 0; i < S::kStages; ++i)
+            for (int spin = 0; spin < (1 << 20); ++spin)
+                if (mbar_try(smem_u32(&s_bar[warp][i]), (phase >> i) & 1)) break;
+    }
+}
+
+template <int FMT, int D, int NT, bool LIST>
+cudaError_t run(const AttendArgs& a, int sms, cudaStream_t st) {
+    using S = Shape<FMT, D, NT>;
+    constexpr int R = S::kRows;
+    auto kernel = attend_kernel<FMT, D, NT, LIST>;
+    static int known[64];                     // per instance and device: CTAs an SM holds
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
+    int occupancy = dev < 64 ? known[dev] : 0;
+    if (occupancy == 0) {
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+        int n = 0;
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kThreads, S::kSmem);
+        if (e != cudaSuccess) return e;
+        occupancy = n > 0 ? n : 1;
+        if (dev < 64) known[dev] = occupancy;
+    }
+    Plan p{};
+    p.per_token = (a.group + R - 1) / R;
+    const int64_t tiles = LIST ? (int64_t)a.b.ntok * p.per_token
+                               : a.b.start ? (int64_t)a.b.ntok * a.group / R + a.b.nreq : (int64_t)a.b.nreq * p.per_token;
+    if (tiles > 0x7FFFFFFFll / 2) return cudaErrorInvalidValue;
+    p.ntiles = (int32_t)tiles;
+    const int64_t slots = (int64_t)sms * occupancy < kMaxCtas ? (int64_t)sms * occupancy : kMaxCtas;
+    // many pairs: one CTA each, balanced by the hardware; fewer: equal shares of the line of units
+    p.whole = LIST ? tiles * a.c.nheads >= 4 * slots : tiles > 8192;
+    if (p.whole) {
+        kernel<<<dim3((unsigned)tiles, a.c.nheads), kThreads, S::kSmem, st>>>(a, p);
+    } else {
+        const int64_t most = LIST ? tiles * a.c.nheads * (((int64_t)a.nselect * a.c.page + kUnit - 1) / kUnit)
+                                  : tiles * a.c.nheads * ((((int64_t)a.b.max_blocks << a.c.page_shift) + kUnit - 1) / kUnit);
+        kernel<<<(unsigned)(most < slots ? most : slots), kThreads, S::kSmem, st>>>(a, p);
+    }
+    return cudaGetLastError();
+}
+
+template <int FMT, int D>
+cudaError_t pick_rows(const AttendArgs& a, int sms, cudaStream_t st) {
+    const bool list = a.blocks != nullptr;
+    // rows that can share a kv head: one token's query heads, or those of several tokens of a request
+    const bool wide = a.group > 8 || (!list && a.b.start != nullptr);
+    if (list) return wide ? run<FMT, D, 2, true>(a, sms, st) : run<FMT, D, 1, true>(a, sms, st);
+    return wide ? run<FMT, D, 2, false>(a, sms, st) : run<FMT, D, 1, false>(a, sms, st);
+}
+
+template <int FMT>
+cudaError_t pick_width(const AttendArgs& a, int sms, cudaStream_t st) {
+    if (a.c.d == 64) return pick_rows<FMT, 64>(a, sms, st);
+    if (a.c.d == 128) return pick_rows<FMT, 128>(a, sms, st);
+    return pick_rows<FMT, 256>(a, sms, st);
 }
 
 }  // namespace
 
-size_t attend_workspace_bytes(int d) { return 256; }
+size_t attend_workspace_bytes(int d) { return (size_t)2 * kMaxCtas * 16 * (d + 2) * 4; }
 
 cudaError_t launch_attend(const AttendArgs& a, cudaStream_t st) {
-    const int64_t rows = (int64_t)a.b.ntok * a.c.nheads * a.group;
-    const unsigned grid = (unsigned)((rows + 3) / 4);
-    if (a.c.d == 64) attend_kernel<2><<<grid, 128, 0, st>>>(a);
-    else if (a.c.d == 128) attend_kernel<4><<<grid, 128, 0, st>>>(a);
-    else attend_kernel<8><<<grid, 128, 0, st>>>(a);
-    return cudaGetLastError();
+    static_assert(256 + kMaxCtas * 4 <= kZeroBytes, "tickets");
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    if (a.c.format == IVFPQ_KV_INT4) return pick_width<IVFPQ_KV_INT4>(a, sms, st);
+    if (a.c.format == IVFPQ_KV_BF16) return pick_width<IVFPQ_KV_BF16>(a, sms, st);
+    return pick_width<IVFPQ_KV_FP16>(a, sms, st);
 }
 
 }  // namespace kv

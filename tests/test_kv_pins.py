@@ -85,6 +85,7 @@ ALL = ("append", "read", "select", "attend")
     ({}, dict(nreq=0), {}, BAD, ALL), ({}, dict(max_blocks=0), {}, BAD, ALL), ({}, dict(table_stride=7), {}, BAD, ALL),
     ({}, dict(block_table=None), {}, BAD, ALL), ({}, dict(seq_len=None), {}, BAD, ALL), ({}, dict(block_table=(1 << 16) + 2), {}, BAD, ALL),
     ({}, dict(max_blocks=lib.IVFPQ_KV_MAX_BLOCKS + 1, table_stride=1 << 20), {}, UNS, ("select",)),
+    ({}, dict(max_blocks=(1 << 24) + 1, table_stride=1 << 30), {}, UNS, ALL),
     ({}, {}, dict(ntok=4), BAD, ALL), ({}, {}, dict(ntok=0), BAD, ALL), ({}, dict(q_start=1 << 16), dict(ntok=(1 << 20) + 1), UNS, ALL),
     ({}, {}, dict(dtype=lib.IVFPQ_KV_INT4), UNS, ALL), ({}, {}, dict(dtype=7), UNS, ALL),
     ({}, {}, dict(p=None), BAD, ("append", "select", "attend")), ({}, {}, dict(p=(1 << 24) + 2), BAD, ("append", "select", "attend")),
