@@ -48,6 +48,17 @@ __device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uin
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The same on accumulators that start at zero.
+template <bool BF>
+__device__ __forceinline__ void mma16816_first(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    const float z = 0.f;
+    if (BF)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                     : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(z));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                     : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(z));
+}
 __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
     uint32_t y;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -87,6 +98,7 @@ __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t n) { asm volati
 __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
@@ -104,10 +116,10 @@ struct Shape {
     static constexpr int kStageKeys = kInt4 ? 32 : 16;
     static constexpr int kSubs = kStageKeys / 16;
     static constexpr int kStageBytes = kInt4 ? kSubs * 18 * D : 16 * D * 2 * 2;
-    static constexpr int kStages = kInt4 ? 4 : (D == 64 ? 4 : 3);
+    static constexpr int kStages = D == 64 ? 4 : 3;
     static constexpr int kRingBytes = kStages * kStageBytes;
     static constexpr int kSmem = kWarps * kRingBytes;
-    static constexpr int kMinCtas = D == 256 ? 1 : (kInt4 && NT == 1 ? 3 : 2);
+    static constexpr int kMinCtas = D == 256 ? 1 : (kInt4 && NT == 1 ? 4 : 2);
     static_assert(kRingBytes >= kRows * (D + 4) * 4, "a warp's ring holds its O");
 };
 
@@ -182,11 +194,12 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
     const uint32_t ring_u = smem_u32(ring);
 
     if (kInt4 && lane == 0) {
-        for (int i = 0; i < S::kStages; ++i) mbar_init(smem_u32(&s_bar[warp][i]), 1);
+        for (int i = 0; i < S::kStages; ++i) mbar_init(smem_u32(&s_bar[warp][i]), S::kSubs);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
-    uint32_t phase = 0;                       // parity bit of every stage of the warp's ring
+    int put = 0, get = 0;                     // slots of the warp's ring: filled next, read next
+    uint32_t parity = 0;                      // of the wait for slot `get`
     bool dead = false;                        // a bounded wait ran out
 
     auto units_of = [&](int t, Tile* tl) -> int {
@@ -268,11 +281,11 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
 
         // ---- 16-key pieces of the warp: piece s covers (virtual) keys (u0 + s / 2) 128 + 32 warp + 16 (s % 2) ----
         const int nsub = (u1 - u0) * 2, nstage = nsub / S::kSubs;
-        int pg_cur = -1, pos_cur = 0, pg_nxt = -1, pos_nxt = 0;
-        auto look = [&](int s, int* pg, int* pos) {
-            *pg = -1;
-            *pos = 0;
-            if (s >= nsub) return;
+        const char *k_cur = nullptr, *k_nxt = nullptr, *v_cur = nullptr, *v_nxt = nullptr;   // where piece (batch, lane) is held
+        int pos_cur = 0, pos_nxt = 0;         // and the position of its first key
+        auto look = [&](int s, const char** kp, const char** vp, int* pos) {
+            *kp = nullptr;
+            if (s >= nsub || dead) return;
             const int vk = (u0 + (s >> 1)) * kUnit + warp * 32 + (s & 1) * 16;
             if (vk >= vlen) return;
             int blk = vk >> c.page_shift;
@@ -280,64 +293,62 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                 blk = list[blk];
                 if (blk < 0 || (int64_t)blk << c.page_shift >= lim_hi) return;
             }
-            *pos = (blk << c.page_shift) + (vk & (c.page - 1));
+            const int tk = vk & (c.page - 1);
+            *pos = (blk << c.page_shift) + tk;
             if (*pos >= lim_hi) return;
-            *pg = page_of(a.b, c, tl.r, blk, status);
+            const int pg = page_of(a.b, c, tl.r, blk, status);
+            if (pg < 0) return;
+            if (kInt4) {
+                *kp = reinterpret_cast<const char*>(record_of(c, pg, head, tk >> 4));
+            } else {
+                *kp = c.k + 2 * (pg * c.ks[0] + head * c.ks[1] + tk * c.ks[2]);
+                *vp = c.v + 2 * (pg * c.vs[0] + head * c.vs[1] + tk * c.vs[2]);
+            }
         };
-        look(lane, &pg_cur, &pos_cur);
-        look(lane + 32, &pg_nxt, &pos_nxt);
-        auto issue = [&](int st) {            // stage st of the segment into its slot
+        look(lane, &k_cur, &v_cur, &pos_cur);
+        look(lane + 32, &k_nxt, &v_nxt, &pos_nxt);
+        auto issue = [&](int st) {            // stage st of the segment into the next slot
             if (st < nstage) {
-                const int slot = st % S::kStages;
-                const int s0 = st * S::kSubs;
-                if (s0 && s0 % 32 == 0) {
-                    pg_cur = pg_nxt;
+                const int s0 = st * S::kSubs, l0 = s0 & 31;
+                if (s0 && l0 == 0) {
+                    k_cur = k_nxt;
+                    v_cur = v_nxt;
                     pos_cur = pos_nxt;
-                    look(s0 + 32 + lane, &pg_nxt, &pos_nxt);
+                    look(s0 + 32 + lane, &k_nxt, &v_nxt, &pos_nxt);
                 }
-                int pg[S::kSubs], pos[S::kSubs];
-#pragma unroll
-                for (int i = 0; i < S::kSubs; ++i) {
-                    pg[i] = __shfl_sync(0xffffffffu, pg_cur, (s0 + i) & 31);
-                    pos[i] = __shfl_sync(0xffffffffu, pos_cur, (s0 + i) & 31);
-                }
+                const uint32_t dst = ring_u + put * S::kStageBytes;
                 if (kInt4) {
-                    if (lane == 0) {
-                        uint32_t bytes = 0;
-#pragma unroll
-                        for (int i = 0; i < S::kSubs; ++i) {
-                            s_info[warp][slot][i] = pg[i] >= 0 && !dead ? pos[i] : -1;
-                            if (pg[i] >= 0) bytes += 18 * D;
-                        }
-                        if (bytes && !dead) {
-                            const uint32_t bar = smem_u32(&s_bar[warp][slot]);
-                            mbar_expect(bar, bytes);
-#pragma unroll
-                            for (int i = 0; i < S::kSubs; ++i)
-                                if (pg[i] >= 0)
-                                    bulk_load(ring_u + slot * S::kStageBytes + i * 18 * D,
-                                              record_of(c, pg[i], head, (pos[i] & (c.page - 1)) >> 4), 18 * D, bar);
+                    // the lanes that know the pieces start their copies
+                    const int i = lane - l0;
+                    if (i >= 0 && i < S::kSubs) {
+                        const uint32_t bar = smem_u32(&s_bar[warp][put]);
+                        s_info[warp][put][i] = k_cur && !dead ? pos_cur : -1;
+                        if (k_cur && !dead) {
+                            mbar_expect(bar, 18 * D);
+                            bulk_load(dst + i * 18 * D, k_cur, 18 * D, bar);
+                        } else {
+                            mbar_arrive(bar);
                         }
                     }
                 } else {
-                    if (lane == 0) s_info[warp][slot][0] = pg[0] >= 0 ? pos[0] : -1;
-                    if (pg[0] >= 0) {
+                    const char* kp = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(k_cur), l0));
+                    const char* vp = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(v_cur), l0));
+                    const int pos = __shfl_sync(0xffffffffu, pos_cur, l0);
+                    if (lane == 0) s_info[warp][put][0] = kp ? pos : -1;
+                    if (kp) {
                         constexpr int CH = D / 8;                         // 16-byte chunks of a row
-                        const int tk = pos[0] & (c.page - 1);
-                        const char* kp = c.k + 2 * (pg[0] * c.ks[0] + head * c.ks[1] + tk * c.ks[2]);
-                        const char* vp = c.v + 2 * (pg[0] * c.vs[0] + head * c.vs[1] + tk * c.vs[2]);
-                        const uint32_t dst = ring_u + slot * S::kStageBytes;
 #pragma unroll
                         for (int i = 0; i < 16 * CH / 32; ++i) {
                             const int x = i * 32 + lane, row = x / CH, ch = x % CH;
                             const uint32_t o = row * (2 * D) + ((ch ^ (row & 7)) * 16);
-                            const bool real = pos[0] + row < lim_hi;
+                            const bool real = pos + row < lim_hi;
                             const int rr = real ? row : 0;
                             cp_async16(dst + o, kp + 2 * (rr * c.ks[2] + ch * 8), real);
                             cp_async16(dst + 16 * D * 2 + o, vp + 2 * (rr * c.vs[2] + ch * 8), real);
                         }
                     }
                 }
+                put = put + 1 == S::kStages ? 0 : put + 1;
             }
             if (!kInt4) cp_async_commit();
         };
@@ -351,7 +362,11 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
         // ---- queries ----
         uint32_t qf[NT][KSTEPS][2];
         float qs[NT][kInt4 ? G : 1][2];       // 4-bit: sums of a column's query elements over each group, times 2^-24
-        float cf[NT][2];                      // factor from products to base-2 logits
+        // factor from products to base-2 logits, positive: a negative scale turns the queries' signs, zero becomes tiny (a masked
+        // product is -infinity and has to stay it)
+        float cf[NT][2];
+        const float fscale = fmaxf(fabsf(a.scale), 1e-30f) * kLog2e;
+        const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
         int lim[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -362,10 +377,10 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
             if (!kInt4) {
 #pragma unroll
                 for (int s = 0; s < KSTEPS; ++s) {
-                    qf[nt][s][0] = real ? *reinterpret_cast<const uint32_t*>(qp + 2 * (16 * s + 2 * lc)) : 0u;
-                    qf[nt][s][1] = real ? *reinterpret_cast<const uint32_t*>(qp + 2 * (16 * s + 8 + 2 * lc)) : 0u;
+                    qf[nt][s][0] = real ? *reinterpret_cast<const uint32_t*>(qp + 2 * (16 * s + 2 * lc)) ^ flip : 0u;
+                    qf[nt][s][1] = real ? *reinterpret_cast<const uint32_t*>(qp + 2 * (16 * s + 8 + 2 * lc)) ^ flip : 0u;
                 }
-                cf[nt][0] = cf[nt][1] = a.scale * kLog2e;
+                cf[nt][0] = cf[nt][1] = fscale;
             } else {
                 // the lane's words (group, half): elements 64 group + 16 lc + 8 half + 0..7, scaled by a power of two to just below 2^15
                 uint4 raw[G][2];
@@ -383,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 const int ex = top > 0.f ? min(max(14 - ((int)(__float_as_uint(top) >> 23) - 127), -100), 100) : 0;
-                const float up = __uint_as_float((uint32_t)(127 + ex) << 23);
+                const float up = __uint_as_float((uint32_t)(127 + ex) << 23 | (flip & 0x80000000u));
                 const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
 #pragma unroll
                 for (int gr = 0; gr < G; ++gr) {
@@ -409,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                     qs[nt][gr][0] = __shfl_sync(0xffffffffu, sum, lc * 8);
                     qs[nt][gr][1] = __shfl_sync(0xffffffffu, sum, lc * 8 + 4);
                 }
-                const float f = a.scale * kLog2e * 16777216.f * down;     // 2^24
+                const float f = fscale * 16777216.f * down;               // 2^24
                 cf[nt][0] = __shfl_sync(0xffffffffu, f, lc * 8);
                 cf[nt][1] = __shfl_sync(0xffffffffu, f, lc * 8 + 4);
             }
@@ -434,11 +449,23 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
         }
 
         for (int st = 0; st < nstage; ++st) {
-            const int slot = st % S::kStages;
             __syncwarp();                     // everybody is done with the slot that is filled next
             issue(st + S::kStages - 1);
-            if (!kInt4) cp_async_wait<S::kStages - 1>();
-            __syncwarp();
+            const int slot = get;
+            get = get + 1 == S::kStages ? 0 : get + 1;
+            if (kInt4) {
+                const uint32_t bar = smem_u32(&s_bar[warp][slot]);
+                bool ok = mbar_try(bar, parity);
+                for (int spin = 0; spin < (1 << 20) && !ok; ++spin) ok = mbar_try(bar, parity);
+                if (get == 0) parity ^= 1;
+                if (!__all_sync(0xffffffffu, ok)) {      // the data never came: no more copies, the flag says so
+                    if (lane == 0) atomicOr(status, kFlagWait);
+                    dead = true;
+                }
+            } else {
+                cp_async_wait<S::kStages - 1>();
+                __syncwarp();
+            }
             int pos[S::kSubs];
             bool any = false;
 #pragma unroll
@@ -447,16 +474,6 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                 any |= pos[i] >= 0;
             }
             if (!any) continue;               // uniform over the warp
-            if (kInt4) {
-                const uint32_t bar = smem_u32(&s_bar[warp][slot]);
-                bool ok = false;
-                for (int spin = 0; spin < (1 << 20) && !ok; ++spin) ok = mbar_try(bar, (phase >> slot) & 1);
-                phase ^= 1u << slot;
-                if (!__all_sync(0xffffffffu, ok)) {      // the data never came: no more copies, the flag says so
-                    if (lane == 0) atomicOr(status, kFlagWait);
-                    dead = true;
-                }
-            }
             const char* buf = ring + slot * S::kStageBytes;
             const uint32_t buf_u = ring_u + slot * S::kStageBytes;
             float p[S::kSubs][NT][4];
@@ -471,10 +488,6 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                         for (int x = 0; x < 4; ++x) p[i][nt][x] = -INFINITY;
                     continue;
                 }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) p[i][nt][x] = 0.f;
                 if (kInt4) {
                     constexpr int GP = D >= 128 ? 2 : 1;                  // groups of a plane
                     const char* rec = buf + i * 18 * D;
@@ -497,16 +510,13 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                             const int gr = pl * GP + g;
                             float acc[NT][4];
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                for (int x = 0; x < 4; ++x) acc[nt][x] = 0.f;
-#pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 const uint32_t x = w0[g * 2 + h], y = w1[g * 2 + h], xs = x >> 8, ys = y >> 8;
                                 const int s = (gr * 2 + h) * 2;
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt) {
-                                    mma16816<false>(acc[nt], x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, qf[nt][s][0], qf[nt][s][1]);
+                                    if (h == 0) mma16816_first<false>(acc[nt], x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, qf[nt][s][0], qf[nt][s][1]);
+                                    else mma16816<false>(acc[nt], x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, qf[nt][s][0], qf[nt][s][1]);
                                     mma16816<false>(acc[nt], xs & 0x000f000fu, ys & 0x000f000fu, xs & 0x00f000f0u, ys & 0x00f000f0u, qf[nt][s + 1][0], qf[nt][s + 1][1]);
                                 }
                             }
@@ -514,10 +524,11 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                             const float2 a1 = __half22float2(*reinterpret_cast<const __half2*>(rec + 16 * D + ((lr + 8) * G + gr) * 4));
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
-                                p[i][nt][0] = fmaf(acc[nt][0], a0.x, fmaf(a0.y, qs[nt][gr][0], p[i][nt][0]));
-                                p[i][nt][1] = fmaf(acc[nt][1], a0.x, fmaf(a0.y, qs[nt][gr][1], p[i][nt][1]));
-                                p[i][nt][2] = fmaf(acc[nt][2], a1.x, fmaf(a1.y, qs[nt][gr][0], p[i][nt][2]));
-                                p[i][nt][3] = fmaf(acc[nt][3], a1.x, fmaf(a1.y, qs[nt][gr][1], p[i][nt][3]));
+                                const bool f0 = gr == 0;      // the first group starts the sum
+                                p[i][nt][0] = fmaf(acc[nt][0], a0.x, f0 ? a0.y * qs[nt][gr][0] : fmaf(a0.y, qs[nt][gr][0], p[i][nt][0]));
+                                p[i][nt][1] = fmaf(acc[nt][1], a0.x, f0 ? a0.y * qs[nt][gr][1] : fmaf(a0.y, qs[nt][gr][1], p[i][nt][1]));
+                                p[i][nt][2] = fmaf(acc[nt][2], a1.x, f0 ? a1.y * qs[nt][gr][0] : fmaf(a1.y, qs[nt][gr][0], p[i][nt][2]));
+                                p[i][nt][3] = fmaf(acc[nt][3], a1.x, f0 ? a1.y * qs[nt][gr][1] : fmaf(a1.y, qs[nt][gr][1], p[i][nt][3]));
                             }
                         }
                     }
@@ -528,13 +539,12 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                         uint32_t f[4];
                         ldmatrix4(f, buf_u + row * (2 * D) + (((2 * s + hi) ^ (row & 7)) * 16));
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma16816<BF>(p[i][nt], f[0], f[1], f[2], f[3], qf[nt][s][0], qf[nt][s][1]);
+                        for (int nt = 0; nt < NT; ++nt) {
+                            if (s == 0) mma16816_first<BF>(p[i][nt], f[0], f[1], f[2], f[3], qf[nt][s][0], qf[nt][s][1]);
+                            else mma16816<BF>(p[i][nt], f[0], f[1], f[2], f[3], qf[nt][s][0], qf[nt][s][1]);
+                        }
                     }
                 }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) p[i][nt][x] *= cf[nt][x & 1];
                 if (pos[i] + 16 > lim_lo) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
@@ -554,7 +564,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                     float y = fmaxf(p[0][nt][x], p[0][nt][x + 2]);
                     if (S::kSubs == 2) y = fmaxf(y, fmaxf(p[S::kSubs - 1][nt][x], p[S::kSubs - 1][nt][x + 2]));
                     top[nt][x] = y;
-                    need |= y > m[nt][x] + kSlack;
+                    need |= fmaf(y, cf[nt][x], -m[nt][x]) > kSlack;
                 }
             if (__any_sync(0xffffffffu, need)) {
 #pragma unroll
@@ -564,7 +574,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                         float y = top[nt][x];
 #pragma unroll
                         for (int s = 4; s < 32; s <<= 1) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, s));
-                        const float mn = fmaxf(m[nt][x], y);
+                        const float mn = fmaxf(m[nt][x], y * cf[nt][x]);
                         const float f = m[nt][x] == mn ? 1.f : ex2(m[nt][x] - mn);
                         m[nt][x] = mn;
                         l[nt][x] *= f;
@@ -581,7 +591,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                 const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
 #pragma unroll
                 for (int i = 0; i < S::kSubs; ++i) {
-                    const float e0 = ex2(p[i][nt][0] - m0), e1 = ex2(p[i][nt][1] - m1), e2 = ex2(p[i][nt][2] - m0), e3 = ex2(p[i][nt][3] - m1);
+                    const float e0 = ex2(fmaf(p[i][nt][0], cf[nt][0], -m0)), e1 = ex2(fmaf(p[i][nt][1], cf[nt][1], -m1));
+                    const float e2 = ex2(fmaf(p[i][nt][2], cf[nt][0], -m0)), e3 = ex2(fmaf(p[i][nt][3], cf[nt][1], -m1));
                     l[nt][0] += e0 + e2;
                     l[nt][1] += e1 + e3;
                     pf[i][nt][0] = movmatrix(pack2<BF>(e0, e1));
@@ -744,41 +755,55 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
             }
             __syncthreads();
             if (s_last) {
+                const int first_slot = 2 * c0 + (total * c0 / ctas != pa ? 1 : 0);
+                auto part = [&](int k, int row) { return (size_t)(k == c0 ? first_slot : 2 * k) * R + row; };
+                for (int row = warp; row < rows; row += kWarps) {          // maximum and sum of a row over the parts
+                    float mx = -INFINITY, ls = 0.f;
+                    for (int k = c0 + lane; k <= c1; k += 32) mx = fmaxf(mx, __ldcg(part_ml + part(k, row) * 2));
+#pragma unroll
+                    for (int s = 16; s; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
+                    for (int k = c0 + lane; k <= c1; k += 32) {
+                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(part_ml + part(k, row) * 2));
+                        if (ml.x != -INFINITY || ml.y != 0.f) ls = fmaf(ex2(ml.x - mx), ml.y, ls);
+                    }
+#pragma unroll
+                    for (int s = 16; s; s >>= 1) ls += __shfl_xor_sync(0xffffffffu, ls, s);
+                    if (lane == 0) {
+                        s_ml[0][row][0] = mx;
+                        s_ml[0][row][1] = ls;
+                    }
+                }
+                __syncthreads();
                 for (int i = tid; i < rows * (D / 4); i += kThreads) {
                     const int row = i / (D / 4), d0 = i % (D / 4) * 4;
-                    float mx = -INFINITY;
+                    const float mx = s_ml[0][row][0];
+                    float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
                     for (int k = c0; k <= c1; ++k) {
-                        const int sl = 2 * k + (k == c0 && total * k / ctas != pa ? 1 : 0);
-                        mx = fmaxf(mx, __ldcg(part_ml + ((size_t)sl * R + row) * 2));
-                    }
-                    float x[4] = {0.f, 0.f, 0.f, 0.f}, ls = 0.f;
-#pragma unroll 4
-                    for (int k = c0; k <= c1; ++k) {
-                        const int sl = 2 * k + (k == c0 && total * k / ctas != pa ? 1 : 0);
-                        const size_t pr = (size_t)sl * R + row;
-                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(part_ml + pr * 2));
+                        const size_t pr = part(k, row);
+                        const float mk = __ldcg(part_ml + pr * 2);
                         const float4 y = __ldcg(reinterpret_cast<const float4*>(part_o + pr * D + d0));
-                        const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - mx);
-                        if (ml.x != -INFINITY || ml.y != 0.f) {
-                            x[0] = fmaf(f, y.x, x[0]);
-                            x[1] = fmaf(f, y.y, x[1]);
-                            x[2] = fmaf(f, y.z, x[2]);
-                            x[3] = fmaf(f, y.w, x[3]);
-                            ls = fmaf(f, ml.y, ls);
-                        }
+                        const float f = mk == -INFINITY ? 0.f : ex2(mk - mx);
+                        x[0] = fmaf(f, y.x, x[0]);
+                        x[1] = fmaf(f, y.y, x[1]);
+                        x[2] = fmaf(f, y.z, x[2]);
+                        x[3] = fmaf(f, y.w, x[3]);
                     }
-                    write_out(row, d0, x, ls, mx);
+                    write_out(row, d0, x, s_ml[0][row][1], mx);
                 }
             }
         }
         at += u1 - u0;
         if (at < end) __syncthreads();        // the rings hold O until here
     }
+    // Every copy was waited for above, unless a wait ran out: then wait once more for all slots, again within a limit.
     if (kInt4 && dead) {
-        // copies may still be on their way into this CTA's memory: wait for them, again within a limit
-        for (int i = 0; i < S::kStages; ++i)
+        for (int i = 0; i < S::kStages; ++i) {
             for (int spin = 0; spin < (1 << 20); ++spin)
-                if (mbar_try(smem_u32(&s_bar[warp][i]), (phase >> i) & 1)) break;
+                if (mbar_try(smem_u32(&s_bar[warp][get]), parity ^ 1)) break;
+            get = get + 1 == S::kStages ? 0 : get + 1;
+            if (get == 0) parity ^= 1;
+        }
     }
 }
 
