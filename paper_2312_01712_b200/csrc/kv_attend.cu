@@ -82,6 +82,13 @@ __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
     asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(a), "r"(b), "r"(c));
     return y;
 }
+// (a & mask) | c in one instruction: c has to be in a register.
+template <uint32_t MASK>
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t c) {
+    uint32_t y;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(a), "n"(MASK), "r"(c));
+    return y;
+}
 __device__ __forceinline__ uint32_t hadd2(uint32_t a, uint32_t b) {
     uint32_t y;
     asm("add.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
@@ -127,6 +134,8 @@ struct Plan {
     int32_t ntiles;          // row tiles (an upper bound where requests have several tokens)
     int32_t per_token;       // tiles of a request with one token, or of a listed token
     int32_t whole;           // 1: one CTA per (tile, kv head), nothing is cut
+    uint32_t magic;          // 0x64006400, two fp16 1024; an argument, so that it is in a register and not folded into a second
+                             // immediate, for which the three-input logic instruction has no room
 };
 
 // Rows of a tile: request, its first row (of n_tokens * group), and how many keys its last row sees.
@@ -178,11 +187,12 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
     constexpr int R = S::kRows, G = D / 64, KSTEPS = D / 16, MT = D / 16;
     extern __shared__ __align__(128) char smem[];
     __shared__ __align__(8) uint64_t s_bar[kWarps][S::kStages];
-    __shared__ int s_info[kWarps][S::kStages][2];
+    __shared__ __align__(8) int s_info[kWarps][S::kStages][2];
     __shared__ float s_ml[kWarps][R][2];
     __shared__ long long s_scan[kWarps + 1];
     __shared__ int s_start[3];
     __shared__ int s_last;
+    __shared__ volatile int s_dead[kWarps];   // a bounded wait of the warp ran out
 
     const Cache& c = a.c;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, lr = lane / 4, lc = lane % 4;
@@ -194,13 +204,13 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
     const uint32_t ring_u = smem_u32(ring);
 
     if (kInt4 && lane == 0) {
-        for (int i = 0; i < S::kStages; ++i) mbar_init(smem_u32(&s_bar[warp][i]), S::kSubs);
+        for (int i = 0; i < S::kStages; ++i) mbar_init(smem_u32(&s_bar[warp][i]), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        s_dead[warp] = 0;
     }
     __syncwarp();
     int put = 0, get = 0;                     // slots of the warp's ring: filled next, read next
     uint32_t parity = 0;                      // of the wait for slot `get`
-    bool dead = false;                        // a bounded wait ran out
 
     auto units_of = [&](int t, Tile* tl) -> int {
         if (!tile_of<R, LIST>(a, plan, t, tl, status)) return 0;
@@ -285,7 +295,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
         int pos_cur = 0, pos_nxt = 0;         // and the position of its first key
         auto look = [&](int s, const char** kp, const char** vp, int* pos) {
             *kp = nullptr;
-            if (s >= nsub || dead) return;
+            *pos = lim_hi;                    // no key: masked throughout
+            if (s >= nsub || (kInt4 && s_dead[warp])) return;
             const int vk = (u0 + (s >> 1)) * kUnit + warp * 32 + (s & 1) * 16;
             if (vk >= vlen) return;
             int blk = vk >> c.page_shift;
@@ -294,10 +305,11 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                 if (blk < 0 || (int64_t)blk << c.page_shift >= lim_hi) return;
             }
             const int tk = vk & (c.page - 1);
-            *pos = (blk << c.page_shift) + tk;
-            if (*pos >= lim_hi) return;
+            const int at0 = (blk << c.page_shift) + tk;
+            if (at0 >= lim_hi) return;
             const int pg = page_of(a.b, c, tl.r, blk, status);
             if (pg < 0) return;
+            *pos = at0;
             if (kInt4) {
                 *kp = reinterpret_cast<const char*>(record_of(c, pg, head, tk >> 4));
             } else {
@@ -318,14 +330,25 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                 }
                 const uint32_t dst = ring_u + put * S::kStageBytes;
                 if (kInt4) {
-                    // the lanes that know the pieces start their copies
-                    const int i = lane - l0;
-                    if (i >= 0 && i < S::kSubs) {
+                    const char* kp = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(k_cur), l0));
+                    int2 pos;
+                    pos.x = __shfl_sync(0xffffffffu, pos_cur, l0);
+                    pos.y = __shfl_sync(0xffffffffu, pos_cur, l0 + 1);
+                    const char* kp2 = nullptr;
+                    if (c.page == 16)                                     // else the second piece follows the first
+                        kp2 = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(k_cur), l0 + 1));
+                    if (lane == 0) {
                         const uint32_t bar = smem_u32(&s_bar[warp][put]);
-                        s_info[warp][put][i] = k_cur && !dead ? pos_cur : -1;
-                        if (k_cur && !dead) {
-                            mbar_expect(bar, 18 * D);
-                            bulk_load(dst + i * 18 * D, k_cur, 18 * D, bar);
+                        const uint32_t n0 = pos.x < lim_hi ? 18 * D : 0, n1 = pos.y < lim_hi ? 18 * D : 0;
+                        *reinterpret_cast<int2*>(s_info[warp][put]) = pos;
+                        if (n0 + n1) {
+                            mbar_expect(bar, n0 + n1);
+                            if (!kp2) {
+                                bulk_load(dst, kp, n0 + n1, bar);
+                            } else {
+                                if (n0) bulk_load(dst, kp, n0, bar);
+                                if (n1) bulk_load(dst + 18 * D, kp2, n1, bar);
+                            }
                         } else {
                             mbar_arrive(bar);
                         }
@@ -334,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                     const char* kp = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(k_cur), l0));
                     const char* vp = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(v_cur), l0));
                     const int pos = __shfl_sync(0xffffffffu, pos_cur, l0);
-                    if (lane == 0) s_info[warp][put][0] = kp ? pos : -1;
+                    if (lane == 0) s_info[warp][put][0] = pos;
                     if (kp) {
                         constexpr int CH = D / 8;                         // 16-byte chunks of a row
 #pragma unroll
@@ -455,25 +478,28 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
             get = get + 1 == S::kStages ? 0 : get + 1;
             if (kInt4) {
                 const uint32_t bar = smem_u32(&s_bar[warp][slot]);
-                bool ok = mbar_try(bar, parity);
-                for (int spin = 0; spin < (1 << 20) && !ok; ++spin) ok = mbar_try(bar, parity);
-                if (get == 0) parity ^= 1;
-                if (!__all_sync(0xffffffffu, ok)) {      // the data never came: no more copies, the flag says so
-                    if (lane == 0) atomicOr(status, kFlagWait);
-                    dead = true;
+                if (!mbar_try(bar, parity)) {
+                    bool ok = false;
+                    for (int spin = s_dead[warp] ? (1 << 20) : 0; spin < (1 << 20) && !ok; ++spin) ok = mbar_try(bar, parity);
+                    if (!ok) {                // the data never came: no more copies, the flag says so
+                        s_dead[warp] = 1;
+                        atomicOr(status, kFlagWait);
+                    }
                 }
+                if (get == 0) parity ^= 1;
+                __syncwarp();
             } else {
                 cp_async_wait<S::kStages - 1>();
                 __syncwarp();
             }
             int pos[S::kSubs];
-            bool any = false;
+            bool none = true;
 #pragma unroll
             for (int i = 0; i < S::kSubs; ++i) {
                 pos[i] = s_info[warp][slot][i];
-                any |= pos[i] >= 0;
+                none = none && pos[i] >= lim_hi;
             }
-            if (!any) continue;               // uniform over the warp
+            if (none) continue;               // uniform over the warp
             const char* buf = ring + slot * S::kStageBytes;
             const uint32_t buf_u = ring_u + slot * S::kStageBytes;
             float p[S::kSubs][NT][4];
@@ -481,13 +507,6 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
             // ---- logits ----
 #pragma unroll
             for (int i = 0; i < S::kSubs; ++i) {
-                if (pos[i] < 0) {
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) p[i][nt][x] = -INFINITY;
-                    continue;
-                }
                 if (kInt4) {
                     constexpr int GP = D >= 128 ? 2 : 1;                  // groups of a plane
                     const char* rec = buf + i * 18 * D;
@@ -603,7 +622,6 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
             // ---- O^T += V^T P^T ----
 #pragma unroll
             for (int i = 0; i < S::kSubs; ++i) {
-                if (pos[i] < 0) continue;
                 if (kInt4) {
                     constexpr int DP = D >= 128 ? 128 : 64, W = DP / 64, GP = DP / 64;
                     const char* rec = buf + i * 18 * D;
@@ -649,8 +667,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                                     for (int oc = 0; oc < 2; ++oc) {
                                         const uint32_t y = q ? x[oc] >> 8 : x[oc];
                                         // fp16 1024 + u and 1024 + 16 u: u exactly, then the group's scale and offset
-                                        const uint32_t u0 = hadd2((y & 0x000f000fu) | 0x64006400u, 0xe400e400u);
-                                        const uint32_t u1h = hfma2((y & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, 0xd400d400u);
+                                        const uint32_t u0 = hadd2(and_or<0x000f000fu>(y, plan.magic), 0xe400e400u);
+                                        const uint32_t u1h = hfma2(and_or<0x00f000f0u>(y, plan.magic), 0x2c002c00u, 0xd400d400u);
                                         f[oc * 2] = hfma2(u0, sc[oc], zr[oc]);
                                         f[oc * 2 + 1] = hfma2(u1h, sc[oc], zr[oc]);
                                     }
@@ -797,7 +815,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
         if (at < end) __syncthreads();        // the rings hold O until here
     }
     // Every copy was waited for above, unless a wait ran out: then wait once more for all slots, again within a limit.
-    if (kInt4 && dead) {
+    if (kInt4 && s_dead[warp]) {
         for (int i = 0; i < S::kStages; ++i) {
             for (int spin = 0; spin < (1 << 20); ++spin)
                 if (mbar_try(smem_u32(&s_bar[warp][get]), parity ^ 1)) break;
@@ -825,6 +843,7 @@ cudaError_t run(const AttendArgs& a, int sms, cudaStream_t st) {
         if (dev < 64) known[dev] = occupancy;
     }
     Plan p{};
+    p.magic = 0x64006400u;
     p.per_token = (a.group + R - 1) / R;
     const int64_t tiles = LIST ? (int64_t)a.b.ntok * p.per_token
                                : a.b.start ? (int64_t)a.b.ntok * a.group / R + a.b.nreq : (int64_t)a.b.nreq * p.per_token;
