@@ -26,9 +26,6 @@ namespace ivfpq {
 namespace kv {
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kThreads = 32 * kWarps;
-constexpr int kUnit = 128;               // keys of a unit: 32 per warp
 constexpr int kMaxCtas = 640;            // CTAs that share work (tickets and partial results in the workspace)
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;
@@ -120,13 +117,16 @@ template <int FMT, int D, int NT>
 struct Shape {
     static constexpr bool kInt4 = FMT == IVFPQ_KV_INT4;
     static constexpr int kRows = 8 * NT;
+    static constexpr int kWarps = kInt4 ? 8 : 4;
+    static constexpr int kThreads = 32 * kWarps;
+    static constexpr int kUnit = 32 * kWarps;          // keys of a unit: 32 per warp
     static constexpr int kStageKeys = kInt4 ? 32 : 16;
     static constexpr int kSubs = kStageKeys / 16;
     static constexpr int kStageBytes = kInt4 ? kSubs * 18 * D : 16 * D * 2 * 2;
     static constexpr int kStages = D == 64 ? 4 : 3;
     static constexpr int kRingBytes = kStages * kStageBytes;
     static constexpr int kSmem = kWarps * kRingBytes;
-    static constexpr int kMinCtas = D == 256 ? 1 : (kInt4 && NT == 1 ? 4 : 2);
+    static constexpr int kMinCtas = kInt4 ? (D == 64 || (D == 128 && NT == 1) ? 2 : 1) : (D == 256 ? 1 : 2);
     static_assert(kRingBytes >= kRows * (D + 4) * 4, "a warp's ring holds its O");
 };
 
@@ -180,17 +180,20 @@ __device__ __forceinline__ bool tile_of(const AttendArgs& a, const Plan& p, int 
 }
 
 template <int FMT, int D, int NT, bool LIST>
-__global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) attend_kernel(AttendArgs a, Plan plan) {
+__global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, NT>::kMinCtas)) attend_kernel(AttendArgs a, Plan plan) {
     using S = Shape<FMT, D, NT>;
     constexpr bool kInt4 = S::kInt4;
     constexpr bool BF = FMT == IVFPQ_KV_BF16;
     constexpr int R = S::kRows, G = D / 64, KSTEPS = D / 16, MT = D / 16;
+    constexpr int kWarps = S::kWarps, kThreads = S::kThreads, kUnit = S::kUnit;
     extern __shared__ __align__(128) char smem[];
     __shared__ __align__(8) uint64_t s_bar[kWarps][S::kStages];
     __shared__ __align__(8) int s_info[kWarps][S::kStages][2];
     __shared__ float s_ml[kWarps][R][2];
     __shared__ long long s_scan[kWarps + 1];
-    __shared__ int s_start[3];
+    // The CTA's place on the line of units, kept out of the registers of the loop over keys.
+    __shared__ struct { long long first, end, total, ctas, at, tile_base; int units, head, u0, u1, t; } s_line_;
+    volatile auto& s_line = s_line_;
     __shared__ int s_last;
     __shared__ volatile int s_dead[kWarps];   // a bounded wait of the warp ran out
 
@@ -224,14 +227,21 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
     long long ctas = 1;                                       // that have a part: none is empty
     int t = 0;
     Tile tl{};
-    int units = 0;
+    // first unit of CTA k's part; in 32 bits where they suffice, since a 64-bit division takes hundreds of cycles
+    auto share = [](long long k, long long total, long long ctas) -> long long {
+        return total < (1 << 21) ? (long long)((unsigned)total * (unsigned)k / (unsigned)ctas) : total * k / ctas;
+    };
+    auto cta_of = [](long long u, long long total, long long ctas) -> int {                   // the CTA whose part holds unit u
+        return total < (1 << 21) ? (int)(((unsigned)(u + 1) * (unsigned)ctas - 1u) / (unsigned)total) : (int)(((u + 1) * ctas - 1) / total);
+    };
     if (plan.whole) {
         t = blockIdx.x;
-        units = units_of(t, &tl);
+        const int units = units_of(t, &tl);
         if (units == 0) return;
         first = (long long)blockIdx.y * units;
         end = first + units;
     } else {
+        // every thread sums a run of tiles; the one whose run holds the CTA's first unit finds the tile
         const int per = (plan.ntiles + kThreads - 1) / kThreads;
         const int t_lo = min(tid * per, plan.ntiles), t_hi = min(t_lo + per, plan.ntiles);
         long long sum = 0;
@@ -241,49 +251,85 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
         }
         sum *= c.nheads;
         long long inc = sum;
+        if (plan.ntiles > 1) {
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += y;
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, inc, o);
+                if (lane >= o) inc += y;
+            }
         }
-        if (lane == 31) s_scan[warp] = inc;
+        if (plan.ntiles > 1 ? lane == 31 : tid == 0) s_scan[warp] = inc;
         __syncthreads();
         long long base = inc - sum;
-        for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) base += s_scan[w];
-            total += s_scan[w];
+        if (plan.ntiles > 1) {
+            for (int w = 0; w < kWarps; ++w) {
+                if (w < warp) base += s_scan[w];
+                total += s_scan[w];
+            }
+        } else {
+            total = s_scan[0];
         }
         ctas = min((long long)gridDim.x, total);
         if (blockIdx.x >= ctas) return;
-        first = total * blockIdx.x / ctas;
-        end = total * (blockIdx.x + 1) / ctas;
-        if (base <= first && first < base + sum) {
-            for (int i = t_lo; i < t_hi; ++i) {
-                Tile x;
-                const long long n = (long long)units_of(i, &x) * c.nheads;
-                if (first < base + n) {
-                    s_start[0] = i;
-                    s_scan[kWarps] = base;
-                    break;
+        first = share(blockIdx.x, total, ctas);
+        end = share(blockIdx.x + 1, total, ctas);
+        if (plan.ntiles > 1) {
+            if (base <= first && first < base + sum) {
+                for (int i = t_lo; i < t_hi; ++i) {
+                    Tile x;
+                    const long long n = (long long)units_of(i, &x) * c.nheads;
+                    if (first < base + n) {
+                        s_line.t = i;
+                        s_scan[kWarps] = base;
+                        break;
+                    }
+                    base += n;
                 }
-                base += n;
             }
+            __syncthreads();
+            t = s_line.t;
+            tile_base = s_scan[kWarps];
         }
-        __syncthreads();
-        t = s_start[0];
-        tile_base = s_scan[kWarps];
-        units = units_of(t, &tl);
     }
 
-    for (long long at = first; at < end;) {
-        while (at >= tile_base + (long long)units * c.nheads) {      // next tile with work
-            tile_base += (long long)units * c.nheads;
-            ++t;
-            units = units_of(t, &tl);
+    if (tid == 0) {
+        s_line.first = first;
+        s_line.end = end;
+        s_line.total = total;
+        s_line.ctas = ctas;
+        s_line.at = first;
+        s_line.tile_base = tile_base;
+        s_line.t = t;
+    }
+    __syncthreads();
+
+    for (;;) {
+        int head, u0, u1;
+        {
+            const long long at = s_line.at, end = s_line.end;
+            long long tile_base = s_line.tile_base;
+            int t = s_line.t, units = units_of(t, &tl);
+            const int t0 = t;
+            while (at >= tile_base + (long long)units * c.nheads) {      // next tile with work
+                tile_base += (long long)units * c.nheads;
+                ++t;
+                units = units_of(t, &tl);
+            }
+            head = (int)((unsigned)(at - tile_base) / (unsigned)units);  // units * heads < 2^31: checked at the launch
+            u0 = (int)(at - tile_base - (long long)head * units);
+            u1 = (int)min((long long)units, u0 + (end - at));
+            __syncthreads();
+            if (tid == 0) {
+                if (t != t0) {
+                    s_line.t = t;
+                    s_line.tile_base = tile_base;
+                }
+                s_line.units = units;
+                s_line.head = head;
+                s_line.u0 = u0;
+                s_line.u1 = u1;
+            }
         }
-        const int head = (int)((at - tile_base) / units);
-        const int u0 = (int)(at - tile_base - (long long)head * units);
-        const int u1 = (int)min((long long)units, u0 + (end - at));
         const int rows = min(R, tl.nrows - tl.row0);
         const int lim_lo = tl.limit(tl.row0, a.group), lim_hi = tl.limit(tl.row0 + rows - 1, a.group);
         const int vlen = LIST ? a.nselect << c.page_shift : lim_hi;
@@ -318,7 +364,6 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
             }
         };
         look(lane, &k_cur, &v_cur, &pos_cur);
-        look(lane + 32, &k_nxt, &v_nxt, &pos_nxt);
         auto issue = [&](int st) {            // stage st of the segment into the next slot
             if (st < nstage) {
                 const int s0 = st * S::kSubs, l0 = s0 & 31;
@@ -330,27 +375,24 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                 }
                 const uint32_t dst = ring_u + put * S::kStageBytes;
                 if (kInt4) {
-                    const char* kp = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(k_cur), l0));
-                    int2 pos;
-                    pos.x = __shfl_sync(0xffffffffu, pos_cur, l0);
-                    pos.y = __shfl_sync(0xffffffffu, pos_cur, l0 + 1);
+                    // pages of 32 tokens and more: the second piece follows the first, and one lane knows all
+                    int second = pos_cur + 16;
                     const char* kp2 = nullptr;
-                    if (c.page == 16)                                     // else the second piece follows the first
-                        kp2 = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(k_cur), l0 + 1));
-                    if (lane == 0) {
+                    if (c.page == 16) {
+                        second = __shfl_down_sync(0xffffffffu, pos_cur, 1);
+                        kp2 = reinterpret_cast<const char*>(__shfl_down_sync(0xffffffffu, reinterpret_cast<unsigned long long>(k_cur), 1));
+                    }
+                    if (lane == l0) {
                         const uint32_t bar = smem_u32(&s_bar[warp][put]);
-                        const uint32_t n0 = pos.x < lim_hi ? 18 * D : 0, n1 = pos.y < lim_hi ? 18 * D : 0;
-                        *reinterpret_cast<int2*>(s_info[warp][put]) = pos;
-                        if (n0 + n1) {
-                            mbar_expect(bar, n0 + n1);
-                            if (!kp2) {
-                                bulk_load(dst, kp, n0 + n1, bar);
-                            } else {
-                                if (n0) bulk_load(dst, kp, n0, bar);
-                                if (n1) bulk_load(dst + 18 * D, kp2, n1, bar);
-                            }
+                        const uint32_t n0 = pos_cur < lim_hi ? 18 * D : 0, n1 = second < lim_hi ? 18 * D : 0;
+                        *reinterpret_cast<int2*>(s_info[warp][put]) = make_int2(pos_cur, second);
+                        if (n0 + n1) mbar_expect(bar, n0 + n1);
+                        else mbar_arrive(bar);
+                        if (!kp2) {
+                            if (n0) bulk_load(dst, k_cur, n0 + n1, bar);
                         } else {
-                            mbar_arrive(bar);
+                            if (n0) bulk_load(dst, k_cur, n0, bar);
+                            if (n1) bulk_load(dst + 18 * D, kp2, n1, bar);
                         }
                     }
                 } else {
@@ -381,6 +423,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < S::kStages - 1; ++i) issue(i);
+        look(lane + 32, &k_nxt, &v_nxt, &pos_nxt);
 
         // ---- queries ----
         uint32_t qf[NT][KSTEPS][2];
@@ -505,72 +548,73 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
             float p[S::kSubs][NT][4];
 
             // ---- logits ----
+            if (kInt4) {
+                constexpr int GP = D >= 128 ? 2 : 1;                      // groups of a plane
 #pragma unroll
-            for (int i = 0; i < S::kSubs; ++i) {
-                if (kInt4) {
-                    constexpr int GP = D >= 128 ? 2 : 1;                  // groups of a plane
-                    const char* rec = buf + i * 18 * D;
+                for (int i = 0; i < S::kSubs; ++i)
 #pragma unroll
                     for (int pl = 0; pl < G / GP; ++pl) {
-                        uint32_t w0[GP * 2], w1[GP * 2];
-                        if (GP == 2) {
-                            const uint4 x = *reinterpret_cast<const uint4*>(rec + pl * 1024 + lane * 16);
-                            const uint4 y = *reinterpret_cast<const uint4*>(rec + pl * 1024 + 512 + lane * 16);
-                            w0[0] = x.x; w0[1] = x.y; w0[GP] = x.z; w0[GP + 1] = x.w;
-                            w1[0] = y.x; w1[1] = y.y; w1[GP] = y.z; w1[GP + 1] = y.w;
-                        } else {
-                            const uint2 x = *reinterpret_cast<const uint2*>(rec + lane * 8);
-                            const uint2 y = *reinterpret_cast<const uint2*>(rec + 256 + lane * 8);
-                            w0[0] = x.x; w0[1] = x.y;
-                            w1[0] = y.x; w1[1] = y.y;
+                        uint32_t w[2][GP * 2];                            // [key row lr, lr + 8][group, half]
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const char* at = buf + i * 18 * D + pl * 1024 + k * (64 * 4 * GP) + lane * (8 * GP);
+                            if (GP == 2) {
+                                const uint4 x = *reinterpret_cast<const uint4*>(at);
+                                w[k][0] = x.x; w[k][1] = x.y; w[k][GP] = x.z; w[k][GP + 1] = x.w;
+                            } else {
+                                const uint2 x = *reinterpret_cast<const uint2*>(at);
+                                w[k][0] = x.x; w[k][1] = x.y;
+                            }
                         }
 #pragma unroll
                         for (int g = 0; g < GP; ++g) {
                             const int gr = pl * GP + g;
                             float acc[NT][4];
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const uint32_t x = w0[g * 2 + h], y = w1[g * 2 + h], xs = x >> 8, ys = y >> 8;
-                                const int s = (gr * 2 + h) * 2;
+                            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) {
-                                    if (h == 0) mma16816_first<false>(acc[nt], x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, qf[nt][s][0], qf[nt][s][1]);
-                                    else mma16816<false>(acc[nt], x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, qf[nt][s][0], qf[nt][s][1]);
-                                    mma16816<false>(acc[nt], xs & 0x000f000fu, ys & 0x000f000fu, xs & 0x00f000f0u, ys & 0x00f000f0u, qf[nt][s + 1][0], qf[nt][s + 1][1]);
+                                for (int q = 0; q < 2; ++q) {
+                                    const uint32_t x = w[0][g * 2 + h] >> (q * 8), y = w[1][g * 2 + h] >> (q * 8);
+                                    const int s = (gr * 2 + h) * 2 + q;
+#pragma unroll
+                                    for (int nt = 0; nt < NT; ++nt) {
+                                        if (h + q == 0) mma16816_first<false>(acc[nt], x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, qf[nt][s][0], qf[nt][s][1]);
+                                        else mma16816<false>(acc[nt], x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, qf[nt][s][0], qf[nt][s][1]);
+                                    }
                                 }
-                            }
-                            const float2 a0 = __half22float2(*reinterpret_cast<const __half2*>(rec + 16 * D + (lr * G + gr) * 4));
-                            const float2 a1 = __half22float2(*reinterpret_cast<const __half2*>(rec + 16 * D + ((lr + 8) * G + gr) * 4));
+                            const char* par = buf + i * 18 * D + 16 * D;
+                            const float2 a0 = __half22float2(*reinterpret_cast<const __half2*>(par + (lr * G + gr) * 4));
+                            const float2 a1 = __half22float2(*reinterpret_cast<const __half2*>(par + ((lr + 8) * G + gr) * 4));
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                const bool f0 = gr == 0;      // the first group starts the sum
-                                p[i][nt][0] = fmaf(acc[nt][0], a0.x, f0 ? a0.y * qs[nt][gr][0] : fmaf(a0.y, qs[nt][gr][0], p[i][nt][0]));
-                                p[i][nt][1] = fmaf(acc[nt][1], a0.x, f0 ? a0.y * qs[nt][gr][1] : fmaf(a0.y, qs[nt][gr][1], p[i][nt][1]));
-                                p[i][nt][2] = fmaf(acc[nt][2], a1.x, f0 ? a1.y * qs[nt][gr][0] : fmaf(a1.y, qs[nt][gr][0], p[i][nt][2]));
-                                p[i][nt][3] = fmaf(acc[nt][3], a1.x, f0 ? a1.y * qs[nt][gr][1] : fmaf(a1.y, qs[nt][gr][1], p[i][nt][3]));
-                            }
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) {
+                                    const float sc = x < 2 ? a0.x : a1.x, z = x < 2 ? a0.y : a1.y;
+                                    p[i][nt][x] = fmaf(acc[nt][x], sc, gr == 0 ? z * qs[nt][gr][x & 1] : fmaf(z, qs[nt][gr][x & 1], p[i][nt][x]));
+                                }
                         }
                     }
-                } else {
-                    const int row = (lane & 7) + ((lane >> 3) & 1) * 8, hi = lane >> 4;
+            } else {
+                const int row = (lane & 7) + ((lane >> 3) & 1) * 8, hi = lane >> 4;
 #pragma unroll
-                    for (int s = 0; s < KSTEPS; ++s) {
-                        uint32_t f[4];
-                        ldmatrix4(f, buf_u + row * (2 * D) + (((2 * s + hi) ^ (row & 7)) * 16));
+                for (int s = 0; s < KSTEPS; ++s) {
+                    uint32_t f[4];
+                    ldmatrix4(f, buf_u + row * (2 * D) + (((2 * s + hi) ^ (row & 7)) * 16));
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            if (s == 0) mma16816_first<BF>(p[i][nt], f[0], f[1], f[2], f[3], qf[nt][s][0], qf[nt][s][1]);
-                            else mma16816<BF>(p[i][nt], f[0], f[1], f[2], f[3], qf[nt][s][0], qf[nt][s][1]);
-                        }
+                    for (int nt = 0; nt < NT; ++nt) {
+                        if (s == 0) mma16816_first<BF>(p[0][nt], f[0], f[1], f[2], f[3], qf[nt][s][0], qf[nt][s][1]);
+                        else mma16816<BF>(p[0][nt], f[0], f[1], f[2], f[3], qf[nt][s][0], qf[nt][s][1]);
                     }
                 }
-                if (pos[i] + 16 > lim_lo) {
+            }
+            if (max(pos[0], pos[S::kSubs - 1]) + 16 > lim_lo) {
+#pragma unroll
+                for (int i = 0; i < S::kSubs; ++i)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int x = 0; x < 4; ++x)
                             if (pos[i] + lr + (x >> 1) * 8 >= lim[nt][x & 1]) p[i][nt][x] = -INFINITY;
-                }
             }
 
             // ---- running maximum ----
@@ -715,8 +759,9 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
                 }
             }
         __syncthreads();
-        const bool cut = u0 > 0 || u1 < units;
-        const int slot0 = 2 * blockIdx.x + (at == first ? 0 : 1);
+        const int part0 = s_line.u0, units = s_line.units;
+        const bool cut = part0 > 0 || s_line.u1 < units;
+        const int slot0 = 2 * blockIdx.x + (s_line.at == s_line.first ? 0 : 1);
         auto write_out = [&](int row, int d0, const float* x, float lsum, float mx) {
             const int rr = tl.row0 + row, j = rr / a.group, g = rr % a.group;
             const int64_t orow = (int64_t)(tl.tok0 + j) * (c.nheads * a.group) + head * a.group + g;
@@ -761,58 +806,64 @@ __global__ void __launch_bounds__(kThreads, (Shape<FMT, D, NT>::kMinCtas)) atten
         }
         if (cut) {
             // CTAs whose part touches this pair; the last one to arrive adds all in order
-            const long long pa = tile_base + (long long)head * units, pz = pa + units - 1;
-            const int c0 = (int)(((pa + 1) * ctas - 1) / total), c1 = (int)(((pz + 1) * ctas - 1) / total);
-            __threadfence();
+            const long long pa = s_line.tile_base + (long long)head * units, pz = pa + units - 1, total = s_line.total, ctas = s_line.ctas;
+            const int c0 = cta_of(pa, total, ctas), c1 = cta_of(pz, total, ctas);
             __syncthreads();
             if (tid == 0) {
-                const int old = atomicAdd(&tickets[c0], 1);
+                // releases the CTA's partial results (ordered before it by the barrier), acquires the others'
+                int old;
+                asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(old) : "l"(tickets + c0) : "memory");
                 s_last = old == c1 - c0;
                 if (s_last) tickets[c0] = 0;
-                __threadfence();
             }
             __syncthreads();
             if (s_last) {
-                const int first_slot = 2 * c0 + (total * c0 / ctas != pa ? 1 : 0);
+                const int first_slot = 2 * c0 + (share(c0, total, ctas) != pa ? 1 : 0);
                 auto part = [&](int k, int row) { return (size_t)(k == c0 ? first_slot : 2 * k) * R + row; };
-                for (int row = warp; row < rows; row += kWarps) {          // maximum and sum of a row over the parts
-                    float mx = -INFINITY, ls = 0.f;
-                    for (int k = c0 + lane; k <= c1; k += 32) mx = fmaxf(mx, __ldcg(part_ml + part(k, row) * 2));
-#pragma unroll
-                    for (int s = 16; s; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
-                    for (int k = c0 + lane; k <= c1; k += 32) {
-                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(part_ml + part(k, row) * 2));
-                        if (ml.x != -INFINITY || ml.y != 0.f) ls = fmaf(ex2(ml.x - mx), ml.y, ls);
-                    }
-#pragma unroll
-                    for (int s = 16; s; s >>= 1) ls += __shfl_xor_sync(0xffffffffu, ls, s);
-                    if (lane == 0) {
-                        s_ml[0][row][0] = mx;
-                        s_ml[0][row][1] = ls;
-                    }
-                }
-                __syncthreads();
+                constexpr int B = 4;                                       // parts whose loads are in flight together
                 for (int i = tid; i < rows * (D / 4); i += kThreads) {
                     const int row = i / (D / 4), d0 = i % (D / 4) * 4;
-                    const float mx = s_ml[0][row][0];
-                    float x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-                    for (int k = c0; k <= c1; ++k) {
-                        const size_t pr = part(k, row);
-                        const float mk = __ldcg(part_ml + pr * 2);
-                        const float4 y = __ldcg(reinterpret_cast<const float4*>(part_o + pr * D + d0));
-                        const float f = mk == -INFINITY ? 0.f : ex2(mk - mx);
-                        x[0] = fmaf(f, y.x, x[0]);
-                        x[1] = fmaf(f, y.y, x[1]);
-                        x[2] = fmaf(f, y.z, x[2]);
-                        x[3] = fmaf(f, y.w, x[3]);
+                    float mx = -INFINITY, ls = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+                    for (int k0 = c0; k0 <= c1; k0 += B) {
+                        float2 ml[B];
+                        float4 y[B];
+#pragma unroll
+                        for (int k = 0; k < B; ++k) {
+                            ml[k] = make_float2(-INFINITY, 0.f);
+                            if (k0 + k <= c1) {
+                                const size_t pr = part(k0 + k, row);
+                                ml[k] = __ldcg(reinterpret_cast<const float2*>(part_ml + pr * 2));
+                                y[k] = __ldcg(reinterpret_cast<const float4*>(part_o + pr * D + d0));
+                            }
+                        }
+                        float mn = mx;
+#pragma unroll
+                        for (int k = 0; k < B; ++k) mn = fmaxf(mn, ml[k].x);
+                        const float f0 = mx == mn ? 1.f : ex2(mx - mn);
+                        mx = mn;
+                        ls *= f0;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[j] *= f0;
+#pragma unroll
+                        for (int k = 0; k < B; ++k) {
+                            if (ml[k].x == -INFINITY && ml[k].y == 0.f) continue;          // a part that saw no key
+                            const float f = ex2(ml[k].x - mx);
+                            ls = fmaf(f, ml[k].y, ls);
+                            x[0] = fmaf(f, y[k].x, x[0]);
+                            x[1] = fmaf(f, y[k].y, x[1]);
+                            x[2] = fmaf(f, y[k].z, x[2]);
+                            x[3] = fmaf(f, y[k].w, x[3]);
+                        }
                     }
-                    write_out(row, d0, x, s_ml[0][row][1], mx);
+                    write_out(row, d0, x, ls, mx);
                 }
             }
         }
-        at += u1 - u0;
-        if (at < end) __syncthreads();        // the rings hold O until here
+        const long long next = s_line.at + (s_line.u1 - part0);
+        if (next >= s_line.end) break;
+        __syncthreads();                      // the rings hold O until here
+        if (tid == 0) s_line.at = next;
+        __syncthreads();
     }
     // Every copy was waited for above, unless a wait ran out: then wait once more for all slots, again within a limit.
     if (kInt4 && s_dead[warp]) {
@@ -837,7 +888,7 @@ cudaError_t run(const AttendArgs& a, int sms, cudaStream_t st) {
     if (occupancy == 0) {
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
         int n = 0;
-        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kThreads, S::kSmem);
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, S::kThreads, S::kSmem);
         if (e != cudaSuccess) return e;
         occupancy = n > 0 ? n : 1;
         if (dev < 64) known[dev] = occupancy;
@@ -849,15 +900,17 @@ cudaError_t run(const AttendArgs& a, int sms, cudaStream_t st) {
                                : a.b.start ? (int64_t)a.b.ntok * a.group / R + a.b.nreq : (int64_t)a.b.nreq * p.per_token;
     if (tiles > 0x7FFFFFFFll / 2) return cudaErrorInvalidValue;
     p.ntiles = (int32_t)tiles;
+    // units of all heads of a tile fit 31 bits
+    if ((((int64_t)(LIST ? a.nselect : a.b.max_blocks) * a.c.page + S::kUnit - 1) / S::kUnit + 1) * a.c.nheads > 0x7FFFFFFFll) return cudaErrorInvalidValue;
     const int64_t slots = (int64_t)sms * occupancy < kMaxCtas ? (int64_t)sms * occupancy : kMaxCtas;
     // many pairs: one CTA each, balanced by the hardware; fewer: equal shares of the line of units
     p.whole = LIST ? tiles * a.c.nheads >= 4 * slots : tiles > 8192;
     if (p.whole) {
-        kernel<<<dim3((unsigned)tiles, a.c.nheads), kThreads, S::kSmem, st>>>(a, p);
+        kernel<<<dim3((unsigned)tiles, a.c.nheads), S::kThreads, S::kSmem, st>>>(a, p);
     } else {
-        const int64_t most = LIST ? tiles * a.c.nheads * (((int64_t)a.nselect * a.c.page + kUnit - 1) / kUnit)
-                                  : tiles * a.c.nheads * ((((int64_t)a.b.max_blocks << a.c.page_shift) + kUnit - 1) / kUnit);
-        kernel<<<(unsigned)(most < slots ? most : slots), kThreads, S::kSmem, st>>>(a, p);
+        const int64_t most = LIST ? tiles * a.c.nheads * (((int64_t)a.nselect * a.c.page + S::kUnit - 1) / S::kUnit)
+                                  : tiles * a.c.nheads * ((((int64_t)a.b.max_blocks << a.c.page_shift) + S::kUnit - 1) / S::kUnit);
+        kernel<<<(unsigned)(most < slots ? most : slots), S::kThreads, S::kSmem, st>>>(a, p);
     }
     return cudaGetLastError();
 }
