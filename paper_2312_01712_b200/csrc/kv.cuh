@@ -169,6 +169,8 @@ struct AttendArgs {
 };
 cudaError_t launch_attend(const AttendArgs& a, cudaStream_t st);
 size_t attend_workspace_bytes(int d);
+bool attend_tile_serves(const AttendArgs& a);      // kv_attend_tile.cu
+cudaError_t launch_attend_tile(const AttendArgs& a, cudaStream_t st);
 
 }  // namespace kv
 }  // namespace ivfpq
