@@ -131,7 +131,8 @@ __device__ __forceinline__ uint4 pack8(const float* x, bool bf16) {
 // What 8 codes of a word stand for (s * u exact in fp32: one rounding).
 __device__ __forceinline__ void decode8(uint32_t w, float s, float z, float* x) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __fmaf_rn(s, (float)((w >> (4 * i)) & 15u), z);
+    for (int i = 0; i < 8; ++i)           // 2^23 + u as bits: no conversion instruction
+        x[i] = __fmaf_rn(s, __uint_as_float(((w >> (4 * i)) & 15u) | 0x4b000000u) - 8388608.f, z);
 }
 
 // 8-bit codes of values of magnitude <= top: rint(x * (127 * (1 / top))), each step rounded to fp32.

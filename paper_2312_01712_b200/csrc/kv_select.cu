@@ -6,7 +6,8 @@
 // straight into the instruction's operand; the order in which the summed axis is dealt to lanes is free, as long as q has the
 // same.  A CTA scores a tile of tokens of one request (one token in a decode step), so that a prompt reads the bounds once per
 // tile, keeps the scores as order-preserving 32-bit keys in shared memory, and finds each token's nselect-th
-// largest key bit by bit: count the keys at or above a candidate, from the highest bit in which keys differ, until the count fits.
+// largest key two bits at a time: count the keys at or above the candidates, from the highest bit in which keys differ, until a count
+// fits.
 // With few rows and many blocks a cluster of CTAs shares a row's blocks and sends its keys to the first one's
 // shared memory.
 #include "kv.cuh"
@@ -57,14 +58,38 @@ struct SelectPlan {
 };
 
 // Writes the n largest of keys[0 .. nb), ties to the lowest index, in ascending order of index.  W warps work together
-// (W = 1: a warp by itself); cnt: [32] zeroed counters, aux: [2 W] words; nb > n >= 1.
-template <int W>
-__device__ __forceinline__ void pick(const uint32_t* keys, int nb, int n, int32_t* out, int warp, int lane, int* cnt, uint32_t* bits, int* aux) {
+// (W = 1: a warp by itself); cnt: [32] zeroed counters, aux: [2 W] words; nb > n >= 1.  Two bits of the n-th largest key are found per
+// pass, by counting the keys at or above three candidates.  NK > 0: a lane's keys, at most NK, stay in registers.
+template <int W, int NK>
+__device__ __forceinline__ void pick(const uint32_t* keys, int nb, int n, int32_t* out, int warp, int lane, unsigned long long* cnt, uint32_t* bits,
+                                     int* aux) {
     auto sync = [] { if (W > 1) __syncthreads(); else __syncwarp(); };
+    uint32_t kr[NK > 0 ? NK : 1];
+    auto each = [&](auto f) {
+        if (NK > 0) {
+#pragma unroll
+            for (int i = 0; i < NK; ++i)
+                if (W * 32 * i < nb) f(kr[i]);     // past the end: key 0, below every candidate
+        } else {
+            for (int i = warp * 32 + lane; i < nb; i += W * 32) f(keys[i]);
+        }
+    };
     uint32_t all = 0xffffffffu, any = 0u;
-    for (int i = warp * 32 + lane; i < nb; i += W * 32) {
-        all &= keys[i];
-        any |= keys[i];
+    if (NK > 0) {
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            const int at = (i * W + warp) * 32 + lane;
+            kr[i] = at < nb ? keys[at] : 0u;
+            if (at < nb) {
+                all &= kr[i];
+                any |= kr[i];
+            }
+        }
+    } else {
+        each([&](uint32_t k) {
+            all &= k;
+            any |= k;
+        });
     }
     all = __reduce_and_sync(0xffffffffu, all);
     any = __reduce_or_sync(0xffffffffu, any);
@@ -79,18 +104,42 @@ __device__ __forceinline__ void pick(const uint32_t* keys, int nb, int n, int32_
     }
     const int high = 31 - __clz(all ^ any);        // -1: all keys are equal
     uint32_t t = high == 31 ? 0u : high < 0 ? all : all & ~((2u << high) - 1u);
-    for (int b = high; b >= 0; --b) {
-        const uint32_t cand = t | (1u << b);
-        int x = 0;
-        for (int i = warp * 32 + lane; i < nb; i += W * 32) x += keys[i] >= cand;
-        x = __reduce_add_sync(0xffffffffu, x);
+    bool exact = false;
+    for (int b = high; b >= 0 && !exact;) {
+        const int lowbit = b > 0 ? b - 1 : 0;      // the pass finds bits b and lowbit (bit 0 alone at the end)
+        const uint32_t c1 = t | (1u << lowbit), c2 = t | (1u << b), c3 = c2 | (1u << lowbit);
+        int n1 = 0, n2 = 0, n3 = 0;
+        each([&](uint32_t k) {
+            n1 += k >= c1;
+            n2 += k >= c2;
+            n3 += k >= c3;
+        });
+        // counts of up to 2^15 + 2^5 keys in 21 bits each
+        unsigned long long x;
+        if (W == 1 && NK > 0) {                    // at most 1024 keys: 11 bits would do, two words of two
+            const uint32_t y = __reduce_add_sync(0xffffffffu, (uint32_t)n1 | (uint32_t)n2 << 16);
+            x = (y & 0xffffu) | (unsigned long long)(y >> 16) << 21 | (unsigned long long)__reduce_add_sync(0xffffffffu, n3) << 42;
+        } else {
+            x = (unsigned long long)__reduce_add_sync(0xffffffffu, n1) | (unsigned long long)__reduce_add_sync(0xffffffffu, n2) << 21 |
+                (unsigned long long)__reduce_add_sync(0xffffffffu, n3) << 42;
+        }
         if (W > 1) {
             if (lane == 0) atomicAdd(&cnt[b], x);
             sync();
             x = cnt[b];
         }
-        if (x >= n) t = cand;
-        if (x == n) break;
+        const int m1 = (int)(x & 0x1fffff), m2 = (int)(x >> 21 & 0x1fffff), m3 = (int)(x >> 42);
+        if (m3 >= n) {
+            t = c3;
+            exact = m3 == n;
+        } else if (m2 >= n) {
+            t = c2;
+            exact = m2 == n;
+        } else if (m1 >= n) {
+            t = c1;
+            exact = m1 == n;
+        }
+        b -= 2;
     }
     // each warp writes from a contiguous range of its own
     const int per = ((nb + W - 1) / W + 31) / 32 * 32, lo = min(warp * per, nb), hi = min(lo + per, nb);
@@ -137,7 +186,7 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, SelectPl
     constexpr int CH = 2 * D / 64;                 // 64-byte segments of a block's bounds
     constexpr int KS = 2 * CH;                     // matrix steps of 32 bytes
     extern __shared__ __align__(16) uint32_t s_key[];       // [tokens][blocks], then the queries' operands
-    __shared__ int s_cnt[32];
+    __shared__ unsigned long long s_cnt[32];
     __shared__ uint32_t s_bits[2];
     __shared__ int s_aux[2 * kWarps];
     const Cache& c = a.c;
@@ -220,14 +269,18 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, SelectPl
         const int g1 = min((rank + 1) * share, groups);
         const uint32_t key0 = p.split > 1 ? in_first_cta(s_key) : 0;
         const int per8 = p.cols < 8 ? 8 / p.cols : 1;                 // tokens of a group of 8 columns
+        auto page_at = [&](int gr, int h) {
+            const int blk = gr * 16 + lr + h * 8;
+            return gr < g1 && blk < nb_max ? page_of(a.b, c, r, blk, a.status) : -1;
+        };
+        int next[2] = {page_at(rank * share + warp, 0), page_at(rank * share + warp, 1)};
         for (int gr = rank * share + warp; gr < g1; gr += kWarps) {
             uint32_t w[2][CH][4];
             float scale[2];
             bool ok[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int blk = gr * 16 + lr + h * 8;
-                const int page = blk < nb_max ? page_of(a.b, c, r, blk, a.status) : -1;
+                const int page = next[h];
                 ok[h] = page >= 0;
                 const int64_t at = (int64_t)max(page, 0) * c.nheads + head;
                 scale[h] = c.scale[at];
@@ -237,6 +290,8 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, SelectPl
                     w[h][i][0] = x.x; w[h][i][1] = x.y; w[h][i][2] = x.z; w[h][i][3] = x.w;
                 }
             }
+            next[0] = page_at(gr + kWarps, 0);     // while the bounds are on their way
+            next[1] = page_at(gr + kWarps, 1);
             int best[4] = {INT_MIN, INT_MIN, INT_MIN, INT_MIN};
             for (int nt = 0; nt < p.ntiles8; ++nt) {
                 int acc[4] = {0, 0, 0, 0};
@@ -297,7 +352,8 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, SelectPl
         if (n == 0) return;
         int32_t* out = a.out + ((int64_t)tok0 * c.nheads + head) * a.nselect;
         if (score) {
-            pick<kWarps>(s_key, nb_max, a.nselect, out, warp, lane, s_cnt, s_bits, s_aux);
+            if (nb_max <= kThreads * 4) pick<kWarps, 4>(s_key, nb_max, a.nselect, out, warp, lane, s_cnt, s_bits, s_aux);
+            else pick<kWarps, 0>(s_key, nb_max, a.nselect, out, warp, lane, s_cnt, s_bits, s_aux);
         } else {
             for (int i = tid; i < a.nselect; i += kThreads) out[i] = i < nb_max ? i : -1;
         }
@@ -306,7 +362,10 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, SelectPl
             int32_t* out = a.out + ((int64_t)(tok0 + j) * c.nheads + head) * a.nselect;
             const int nb = blocks_of(j);
             if (nb > a.nselect) {
-                pick<1>(s_key + (size_t)j * stride, nb, a.nselect, out, 0, lane, nullptr, nullptr, nullptr);
+                const uint32_t* keys = s_key + (size_t)j * stride;
+                if (nb <= 32 * 8) pick<1, 8>(keys, nb, a.nselect, out, 0, lane, nullptr, nullptr, nullptr);
+                else if (nb <= 32 * 24) pick<1, 24>(keys, nb, a.nselect, out, 0, lane, nullptr, nullptr, nullptr);
+                else pick<1, 0>(keys, nb, a.nselect, out, 0, lane, nullptr, nullptr, nullptr);
             } else {
                 for (int i = lane; i < a.nselect; i += 32) out[i] = i < nb ? i : -1;
             }
