@@ -5,10 +5,8 @@
 // (token, query head) columns, 32-bit sums: exact in any order).  A lane reads 16 consecutive bytes of a block's bounds
 // straight into the instruction's operand; the order in which the summed axis is dealt to lanes is free, as long as q has the
 // same.  A CTA scores a tile of tokens of one request (one token in a decode step), so that a prompt reads the bounds once per
-// tile, keeps the scores as order-preserving 32-bit keys in shared memory, and finds each token's nselect-th
-// largest key two bits at a time: count the keys at or above the candidates, from the highest bit in which keys differ, until a count
-// fits.
-// With few rows and many blocks a cluster of CTAs shares a row's blocks and sends its keys to the first one's
+// tile, keeps the scores in shared memory, and finds each token's nselect best by a histogram (see pick).
+// With few rows and many blocks a cluster of CTAs shares a row's blocks and sends its scores to the first one's
 // shared memory.
 #include "kv.cuh"
 
@@ -57,149 +55,185 @@ struct SelectPlan {
     int32_t ntiles8;         // groups of 8 columns in all
 };
 
-// Writes the n largest of keys[0 .. nb), ties to the lowest index, in ascending order of index.  W warps work together
-// (W = 1: a warp by itself); cnt: [32] zeroed counters, aux: [2 W] words; nb > n >= 1.  Two bits of the n-th largest key are found per
-// pass, by counting the keys at or above three candidates.  NK > 0: a lane's keys, at most NK, stay in registers.
-template <int W, int NK>
-__device__ __forceinline__ void pick(const uint32_t* keys, int nb, int n, int32_t* out, int warp, int lane, unsigned long long* cnt, uint32_t* bits,
-                                     int* aux) {
+// (score, block) as one number: larger is better, ties to the lower block.
+__device__ __forceinline__ unsigned long long rank_key(float s, int blk) { return (unsigned long long)score_key(s) << 32 | (uint32_t)~blk; }
+
+// Threshold by bits, for many equal or nearly equal scores: the n-th largest rank key, found from the highest bit down by counting.
+template <int W>
+__device__ __noinline__ unsigned long long threshold_by_bits(const float* sc, int nb, int n, int warp, int lane, int* count) {
     auto sync = [] { if (W > 1) __syncthreads(); else __syncwarp(); };
-    uint32_t kr[NK > 0 ? NK : 1];
-    auto each = [&](auto f) {
+    unsigned long long t = 0ull;
+    for (int b = 63; b >= 0; --b) {
+        const unsigned long long cand = t | 1ull << b;
+        int x = 0;
+        for (int i = warp * 32 + lane; i < nb; i += W * 32) x += rank_key(sc[i], i) >= cand;
+        x = __reduce_add_sync(0xffffffffu, x);
+        if (W > 1) {
+            sync();
+            if (warp == 0 && lane == 0) count[0] = 0;
+            sync();
+            if (lane == 0) atomicAdd(&count[0], x);
+            sync();
+            x = count[0];
+        }
+        if (x >= n) t = cand;
+        if (x == n) break;
+    }
+    return t;
+}
+
+// Scratch of a pick by W warps.
+template <int W>
+struct PickShared {
+    static constexpr int kBuckets = 128 * W;
+    int hist[kBuckets];
+    unsigned long long list[32 * W];
+    unsigned long long cut;
+    int aux[2 * W], sums[W];
+    int bucket, above, fill, count;
+};
+
+// Writes the n best of the scores sc[0 .. nb) as ascending indices; W warps work together (W = 1: a warp by itself); nb > n >= 1.
+// One pass counts the scores in equal buckets between the smallest and the largest finite one, a scan from the top finds the bucket of the
+// n-th best, and only that bucket's few scores are ranked exactly, each against all.  Buckets follow the score, so any distribution gives the
+// same answer; one that crowds a bucket (more than 32 W in it) takes the threshold by bits instead.
+// NK > 0: a lane's scores, at most NK, stay in registers, and the passes over them are unrolled.
+template <int W, int NK>
+__device__ __forceinline__ void pick(const float* sc, int nb, int n, int32_t* out, int warp, int lane, PickShared<W>& sh) {
+    constexpr int NB = PickShared<W>::kBuckets, T = 32 * W;
+    auto sync = [] { if (W > 1) __syncthreads(); else __syncwarp(); };
+    const int id = warp * 32 + lane;
+    // a warp's scores are a contiguous range, so that its part of the list is one as well
+    const int per = ((nb + W - 1) / W + 31) / 32 * 32, lo = min(warp * per, nb), hi = min(lo + per, nb);
+    float fr[NK > 0 ? NK : 1];
+    if (NK > 0) {
+#pragma unroll
+        for (int i = 0; i < NK; ++i) fr[i] = lo + i * 32 + lane < hi ? sc[lo + i * 32 + lane] : -INFINITY;
+    }
+    auto each = [&](auto f) {                      // f(score, its index, whether there is one): whole warps
         if (NK > 0) {
 #pragma unroll
             for (int i = 0; i < NK; ++i)
-                if (W * 32 * i < nb) f(kr[i]);     // past the end: key 0, below every candidate
+                if (lo + i * 32 < hi) f(fr[i], lo + i * 32 + lane, lo + i * 32 + lane < hi);
         } else {
-            for (int i = warp * 32 + lane; i < nb; i += W * 32) f(keys[i]);
+            for (int i = lo + lane; i - lane < hi; i += 32) f(i < hi ? sc[i] : -INFINITY, i, i < hi);
         }
     };
-    uint32_t all = 0xffffffffu, any = 0u;
-    if (NK > 0) {
-#pragma unroll
-        for (int i = 0; i < NK; ++i) {
-            const int at = (i * W + warp) * 32 + lane;
-            kr[i] = at < nb ? keys[at] : 0u;
-            if (at < nb) {
-                all &= kr[i];
-                any |= kr[i];
-            }
+    float top = -INFINITY, low = INFINITY;         // of the finite scores: forced blocks do not stretch the range
+    each([&](float f, int, bool) {
+        if (fabsf(f) < INFINITY) {
+            top = fmaxf(top, f);
+            low = fminf(low, f);
+        }
+    });
+    uint32_t utop = __reduce_max_sync(0xffffffffu, score_key(top)), ulow = __reduce_min_sync(0xffffffffu, score_key(low));
+    for (int i = id; i < NB; i += T) sh.hist[i] = 0;
+    if (W > 1) {
+        if (lane == 0) {
+            sh.aux[warp] = (int)utop;
+            sh.aux[W + warp] = (int)ulow;
+        }
+        if (id == 0) sh.fill = 0;
+        sync();
+        for (int w = 0; w < W; ++w) {
+            utop = max(utop, (uint32_t)sh.aux[w]);
+            ulow = min(ulow, (uint32_t)sh.aux[W + w]);
         }
     } else {
-        each([&](uint32_t k) {
-            all &= k;
-            any |= k;
-        });
-    }
-    all = __reduce_and_sync(0xffffffffu, all);
-    any = __reduce_or_sync(0xffffffffu, any);
-    if (W > 1) {
-        if (lane == 0) {
-            atomicAnd(&bits[0], all);
-            atomicOr(&bits[1], any);
-        }
+        if (id == 0) sh.fill = 0;
         sync();
-        all = bits[0];
-        any = bits[1];
     }
-    const int high = 31 - __clz(all ^ any);        // -1: all keys are equal
-    uint32_t t = high == 31 ? 0u : high < 0 ? all : all & ~((2u << high) - 1u);
-    bool exact = false;
-    for (int b = high; b >= 0 && !exact;) {
-        const int lowbit = b > 0 ? b - 1 : 0;      // the pass finds bits b and lowbit (bit 0 alone at the end)
-        const uint32_t c1 = t | (1u << lowbit), c2 = t | (1u << b), c3 = c2 | (1u << lowbit);
-        int n1 = 0, n2 = 0, n3 = 0;
-        each([&](uint32_t k) {
-            n1 += k >= c1;
-            n2 += k >= c2;
-            n3 += k >= c3;
-        });
-        // counts of up to 2^15 + 2^5 keys in 21 bits each
-        unsigned long long x;
-        if (W == 1 && NK > 0) {                    // at most 1024 keys: 11 bits would do, two words of two
-            const uint32_t y = __reduce_add_sync(0xffffffffu, (uint32_t)n1 | (uint32_t)n2 << 16);
-            x = (y & 0xffffu) | (unsigned long long)(y >> 16) << 21 | (unsigned long long)__reduce_add_sync(0xffffffffu, n3) << 42;
-        } else {
-            x = (unsigned long long)__reduce_add_sync(0xffffffffu, n1) | (unsigned long long)__reduce_add_sync(0xffffffffu, n2) << 21 |
-                (unsigned long long)__reduce_add_sync(0xffffffffu, n3) << 42;
-        }
-        if (W > 1) {
-            if (lane == 0) atomicAdd(&cnt[b], x);
-            sync();
-            x = cnt[b];
-        }
-        const int m1 = (int)(x & 0x1fffff), m2 = (int)(x >> 21 & 0x1fffff), m3 = (int)(x >> 42);
-        if (m3 >= n) {
-            t = c3;
-            exact = m3 == n;
-        } else if (m2 >= n) {
-            t = c2;
-            exact = m2 == n;
-        } else if (m1 >= n) {
-            t = c1;
-            exact = m1 == n;
-        }
-        b -= 2;
+    auto value = [](uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); };
+    const float fl = ulow <= utop ? value(ulow) : 0.f, fh = ulow <= utop ? value(utop) : 0.f;
+    const float mul = (float)(NB - 1) / fmaxf((fh - fl) * 1.0000002f, 1e-30f);      // an infinite width: bucket 0 for all
+    auto bucket = [&](float f) {                   // never decreases with f; NaN: 0
+        const float x = fmaxf((fminf(fmaxf(f, fl), fh) - fl) * mul, 0.f);
+        return min((int)(__float_as_uint(x + 8388608.f) & 0x7fffffu), NB - 1);
+    };
+    each([&](float f, int, bool real) { if (real) atomicAdd(&sh.hist[bucket(f)], 1); });
+    sync();
+    // 4 buckets a lane, the highest first
+    int h[4], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += h[i] = sh.hist[NB - 1 - (id * 4 + i)];
+    int inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
     }
-    // each warp writes from a contiguous range of its own
-    const int per = ((nb + W - 1) / W + 31) / 32 * 32, lo = min(warp * per, nb), hi = min(lo + per, nb);
-    int gt = 0, eq = 0;
-    for (int i = lo + lane; i < hi; i += 32) {
-        gt += keys[i] > t;
-        eq += keys[i] == t;
-    }
-    gt = __reduce_add_sync(0xffffffffu, gt);
-    eq = __reduce_add_sync(0xffffffffu, eq);
-    int gt_before = 0, eq_before = 0, gt_all = gt;
     if (W > 1) {
-        if (lane == 0) {
-            aux[warp * 2] = gt;
-            aux[warp * 2 + 1] = eq;
-        }
+        if (lane == 31) sh.sums[warp] = inc;
         sync();
-        gt_all = 0;
-        for (int w = 0; w < W; ++w) {
-            gt_all += aux[w * 2];
-            if (w < warp) {
-                gt_before += aux[w * 2];
-                eq_before += aux[w * 2 + 1];
+        for (int w = 0; w < W; ++w)
+            if (w < warp) inc += sh.sums[w];
+    }
+    if (inc - sum < n && n <= inc) {               // one lane
+        int above = inc - sum, i = 0;
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            if (i == k && above + h[k] < n) {
+                above += h[k];
+                ++i;
             }
-        }
+        sh.bucket = NB - 1 - (id * 4 + i);
+        sh.above = above;
     }
-    const int need = n - gt_all;                   // how many of the equal keys are in
-    int at = gt_before + min(eq_before, need), ties = eq_before;
+    sync();
+    const int bk = sh.bucket, need = n - sh.above, members = sh.hist[bk];
+    unsigned long long cut;
+    if (members <= T) {
+        each([&](float f, int i, bool real) {
+            if (real && bucket(f) == bk) sh.list[atomicAdd(&sh.fill, 1)] = rank_key(f, i);
+        });
+        sync();
+        if (id < members) {
+            const unsigned long long me = sh.list[id];
+            int better = 0;
+            for (int i = 0; i < members; ++i) better += sh.list[i] > me;
+            if (better == need - 1) sh.cut = me;
+        }
+        sync();
+        cut = sh.cut;
+    } else {
+        cut = threshold_by_bits<W>(sc, nb, n, warp, lane, &sh.count);
+    }
+    int at = 0;
+    if (W > 1) {
+        int in = 0;
+        each([&](float f, int i, bool real) { in += real && rank_key(f, i) >= cut; });
+        in = __reduce_add_sync(0xffffffffu, in);
+        if (lane == 0) sh.aux[warp] = in;
+        sync();
+        for (int w = 0; w < W; ++w)
+            if (w < warp) at += sh.aux[w];
+    }
     const unsigned below = (1u << lane) - 1u;
-    for (int i0 = lo; i0 < hi; i0 += 32) {
-        const int i = i0 + lane;
-        const uint32_t k = i < hi ? keys[i] : 0u;
-        const unsigned me = __ballot_sync(0xffffffffu, i < hi && k == t);
-        const bool in = i < hi && (k > t || (k == t && ties + __popc(me & below) < need));
+    each([&](float f, int i, bool real) {
+        const bool in = real && rank_key(f, i) >= cut;
         const unsigned mi = __ballot_sync(0xffffffffu, in);
         if (in) out[at + __popc(mi & below)] = i;
         at += __popc(mi);
-        ties += __popc(me);
-    }
+    });
+    sync();                                        // before the scratch is used again
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, SelectPlan p) {
+// CG: columns of a token, 8 for 8 and more.
+template <int D, int CG>
+__global__ void __launch_bounds__(kThreads, D == 256 ? 2 : 4) select_kernel(SelectArgs a, SelectPlan p) {
     constexpr int CH = 2 * D / 64;                 // 64-byte segments of a block's bounds
     constexpr int KS = 2 * CH;                     // matrix steps of 32 bytes
-    extern __shared__ __align__(16) uint32_t s_key[];       // [tokens][blocks], then the queries' operands
-    __shared__ unsigned long long s_cnt[32];
-    __shared__ uint32_t s_bits[2];
-    __shared__ int s_aux[2 * kWarps];
+    extern __shared__ __align__(16) float s_score[];         // [tokens][blocks], then the queries' operands
+    __shared__ union {
+        PickShared<1> warp[kWarps];
+        PickShared<kWarps> all;
+    } s_pick;
     const Cache& c = a.c;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, lr = lane / 4, lc = lane % 4;
     const int head = blockIdx.y, tile = blockIdx.x / p.split, rank = p.split > 1 ? (int)cluster_rank() : 0;
     const int stride = a.b.max_blocks;
-    uint32_t* s_q = s_key + (((size_t)p.tokens * stride + 3) & ~(size_t)3);        // [columns / 8][KS][lane][2]
+    uint32_t* s_q = reinterpret_cast<uint32_t*>(s_score) + (((size_t)p.tokens * stride + 3) & ~(size_t)3);        // [columns / 8][KS][lane][2]
     if (p.split > 1) cluster_arrive();             // all CTAs of the cluster run before anybody stores to the first
-    if (tid < 32) s_cnt[tid] = 0;
-    if (tid == 0) {
-        s_bits[0] = 0xffffffffu;
-        s_bits[1] = 0u;
-    }
 
     // ---- the tile's tokens: request r, rows tok0 .. tok0 + n, at positions pos0 ... ----
     int r = tile, j0 = 0;
@@ -267,8 +301,7 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, SelectPl
         // ---- scores of 16 blocks per warp and step ----
         const int groups = (nb_max + 15) / 16, share = (groups + p.split - 1) / p.split;
         const int g1 = min((rank + 1) * share, groups);
-        const uint32_t key0 = p.split > 1 ? in_first_cta(s_key) : 0;
-        const int per8 = p.cols < 8 ? 8 / p.cols : 1;                 // tokens of a group of 8 columns
+        const uint32_t first = p.split > 1 ? in_first_cta(s_score) : 0;
         auto page_at = [&](int gr, int h) {
             const int blk = gr * 16 + lr + h * 8;
             return gr < g1 && blk < nb_max ? page_of(a.b, c, r, blk, a.status) : -1;
@@ -281,9 +314,9 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, SelectPl
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int page = next[h];
-                ok[h] = page >= 0;
+                ok[h] = gr * 16 + lr + h * 8 < nb_max;
                 const int64_t at = (int64_t)max(page, 0) * c.nheads + head;
-                scale[h] = c.scale[at];
+                scale[h] = page >= 0 ? c.scale[at] : __int_as_float(0x7fffffff);      // a page outside the cache: NaN, ranks last
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
                     const uint4 x = __ldg(reinterpret_cast<const uint4*>(c.bounds + at * 2 * D + i * 64 + lc * 16));
@@ -292,50 +325,63 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, SelectPl
             }
             next[0] = page_at(gr + kWarps, 0);     // while the bounds are on their way
             next[1] = page_at(gr + kWarps, 1);
-            int best[4] = {INT_MIN, INT_MIN, INT_MIN, INT_MIN};
-            for (int nt = 0; nt < p.ntiles8; ++nt) {
-                int acc[4] = {0, 0, 0, 0};
-                const uint32_t* q = s_q + (nt * KS * 32 + lane) * 2;
+            int best[2] = {INT_MIN, INT_MIN}, left = p.cols / 8, tok = 0;
+            for (int nt2 = 0; nt2 < p.ntiles8; nt2 += 2) {
+              int pair[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+              const uint32_t* q = s_q + (nt2 * KS * 32 + lane) * 2;
 #pragma unroll
-                for (int i = 0; i < CH; ++i)
+              for (int i = 0; i < CH; ++i)
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        const uint2 b = *reinterpret_cast<const uint2*>(q + (i * 2 + s) * 64);
-                        const uint32_t f[4] = {w[0][i][2 * s], w[1][i][2 * s], w[0][i][2 * s + 1], w[1][i][2 * s + 1]};
-                        mma_s8(acc, f, b.x, b.y);
+                for (int s = 0; s < 2; ++s) {
+                    const uint32_t f[4] = {w[0][i][2 * s], w[1][i][2 * s], w[0][i][2 * s + 1], w[1][i][2 * s + 1]};
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const uint2 b = *reinterpret_cast<const uint2*>(q + (u * KS + i * 2 + s) * 64);
+                        mma_s8(pair[u], f, b.x, b.y);
                     }
-                if (p.cols >= 2) {
+                }
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                const int nt = nt2 + u;
+                int* acc = pair[u];
+                if (nt >= p.ntiles8) break;
+                if (CG >= 2) {
                     acc[0] = max(acc[0], acc[1]);
                     acc[2] = max(acc[2], acc[3]);
                 }
-                if (p.cols >= 4) {
+                if (CG >= 4) {
                     acc[0] = max(acc[0], __shfl_xor_sync(0xffffffffu, acc[0], 1));
                     acc[2] = max(acc[2], __shfl_xor_sync(0xffffffffu, acc[2], 1));
                 }
-                if (p.cols >= 8) {
+                int j;                                                // the lane's token of these columns
+                bool writer = true;
+                if (CG == 8) {
                     acc[0] = max(acc[0], __shfl_xor_sync(0xffffffffu, acc[0], 2));
                     acc[2] = max(acc[2], __shfl_xor_sync(0xffffffffu, acc[2], 2));
                     best[0] = max(best[0], acc[0]);
-                    best[2] = max(best[2], acc[2]);
-                    if ((nt + 1) % (p.cols / 8)) continue;            // more of this token's heads follow
+                    best[1] = max(best[1], acc[2]);
+                    if (--left) continue;                             // more of this token's heads follow
                     acc[0] = best[0];
-                    acc[2] = best[2];
-                    best[0] = best[2] = INT_MIN;
+                    acc[2] = best[1];
+                    best[0] = best[1] = INT_MIN;
+                    left = p.cols / 8;
+                    j = tok++;
+                    writer = lc == 0;
+                } else {
+                    j = nt * (8 / CG) + (CG == 4 ? lc / 2 : CG == 2 ? lc : lc * 2);
+                    if (CG == 4) writer = lc % 2 == 0;
                 }
-                const int j = p.cols >= 8 ? nt / (p.cols / 8) : nt * per8 + (p.cols == 4 ? lc / 2 : p.cols == 2 ? lc : lc * 2);
-                const bool writer = p.cols >= 8 ? lc == 0 : p.cols == 4 ? lc % 2 == 0 : true;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    if (x % 2 && p.cols > 1) continue;
-                    const int jj = j + x % 2, h = x / 2, blk = gr * 16 + lr + h * 8;
-                    if (!writer || jj >= n) continue;
-                    const int nb = blocks_of(jj);
-                    if (blk >= nb) continue;
-                    uint32_t key = ok[h] ? score_key(__fmul_rn((float)acc[x], scale[h])) : 0u;
-                    if (blk < a.nsink || blk >= nb - a.nlocal) key = 0xffffffffu;
-                    if (p.split > 1) store_cluster(key0 + ((uint32_t)jj * stride + blk) * 4, key);
-                    else s_key[(size_t)jj * stride + blk] = key;
+                    if (x % 2 && CG > 1) continue;
+                    const int jj = j + x % 2, h = x / 2;
+                    if (!writer || jj >= n || !ok[h]) continue;
+                    const int at = jj * stride + gr * 16 + lr + h * 8;
+                    const float v = __fmul_rn((float)acc[x], scale[h]);
+                    if (p.split > 1) store_cluster(first + (uint32_t)at * 4, __float_as_uint(v));
+                    else s_score[at] = v;
                 }
+              }
             }
         }
     }
@@ -347,13 +393,18 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, SelectPl
         __syncthreads();
     }
 
-    // ---- the lists ----
+    // ---- the lists; blocks that are always in score infinity ----
+    auto force = [&](float* sc, int nb, int i, int step) {
+        for (; i < a.nsink + a.nlocal; i += step) sc[i < a.nsink ? i : nb - 1 - (i - a.nsink)] = INFINITY;
+    };
     if (p.tokens == 1) {
         if (n == 0) return;
         int32_t* out = a.out + ((int64_t)tok0 * c.nheads + head) * a.nselect;
         if (score) {
-            if (nb_max <= kThreads * 4) pick<kWarps, 4>(s_key, nb_max, a.nselect, out, warp, lane, s_cnt, s_bits, s_aux);
-            else pick<kWarps, 0>(s_key, nb_max, a.nselect, out, warp, lane, s_cnt, s_bits, s_aux);
+            force(s_score, nb_max, tid, kThreads);
+            __syncthreads();
+            if (nb_max <= kThreads * 4) pick<kWarps, 4>(s_score, nb_max, a.nselect, out, warp, lane, s_pick.all);
+            else pick<kWarps, 0>(s_score, nb_max, a.nselect, out, warp, lane, s_pick.all);
         } else {
             for (int i = tid; i < a.nselect; i += kThreads) out[i] = i < nb_max ? i : -1;
         }
@@ -362,10 +413,11 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, SelectPl
             int32_t* out = a.out + ((int64_t)(tok0 + j) * c.nheads + head) * a.nselect;
             const int nb = blocks_of(j);
             if (nb > a.nselect) {
-                const uint32_t* keys = s_key + (size_t)j * stride;
-                if (nb <= 32 * 8) pick<1, 8>(keys, nb, a.nselect, out, 0, lane, nullptr, nullptr, nullptr);
-                else if (nb <= 32 * 24) pick<1, 24>(keys, nb, a.nselect, out, 0, lane, nullptr, nullptr, nullptr);
-                else pick<1, 0>(keys, nb, a.nselect, out, 0, lane, nullptr, nullptr, nullptr);
+                float* sc = s_score + (size_t)j * stride;
+                force(sc, nb, lane, 32);
+                __syncwarp();
+                if (nb <= 32 * 16) pick<1, 16>(sc, nb, a.nselect, out, 0, lane, s_pick.warp[warp]);
+                else pick<1, 0>(sc, nb, a.nselect, out, 0, lane, s_pick.warp[warp]);
             } else {
                 for (int i = lane; i < a.nselect; i += 32) out[i] = i < nb ? i : -1;
             }
@@ -373,18 +425,19 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectArgs a, SelectPl
     }
 }
 
-template <int D>
+template <int D, int CG>
 cudaError_t run(const SelectArgs& a, int sms, cudaStream_t st) {
     SelectPlan p{};
     p.cols = a.group <= 2 ? a.group : a.group <= 4 ? 4 : (a.group + 7) / 8 * 8;
     auto bytes = [&](int tokens) {
-        return (((size_t)tokens * a.b.max_blocks + 3) & ~(size_t)3) * 4 + (size_t)((tokens * p.cols + 7) / 8) * 8 * 2 * D;
+        return (((size_t)tokens * a.b.max_blocks + 3) & ~(size_t)3) * 4 + (size_t)((tokens * p.cols + 15) / 16) * 16 * 2 * D;
     };
-    // a prompt: as many tokens per tile as two CTAs an SM have room for, and as leave every SM two CTAs
+    // a prompt: as many tokens per tile as leave room for four CTAs an SM (2048 tokens x 8 heads, 512 blocks: 32 tokens and two
+    // CTAs 100 us, 16 tokens and four 85 us), and as leave every SM two CTAs
     p.tokens = 1;
     if (a.b.start && a.b.ntok >= 4 * (int64_t)a.b.nreq) {
         for (int t = kMaxTokens; t >= 8; t /= 2) {
-            if (bytes(t) > 100 * 1024) continue;
+            if (bytes(t) > 56 * 1024) continue;
             p.tokens = t;
             if (((int64_t)a.b.ntok / t + 1) * a.c.nheads >= 2 * sms) break;
         }
@@ -395,7 +448,7 @@ cudaError_t run(const SelectArgs& a, int sms, cudaStream_t st) {
     p.split = 1;
     while (p.split < 8 && p.tokens == 1 && tiles * a.c.nheads * p.split * 2 <= 2 * sms && a.b.max_blocks >= 256 * p.split) p.split *= 2;
     const size_t smem = bytes(p.tokens);
-    auto kernel = select_kernel<D>;
+    auto kernel = select_kernel<D, CG>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
@@ -412,6 +465,14 @@ cudaError_t run(const SelectArgs& a, int sms, cudaStream_t st) {
     return cudaLaunchKernelEx(&cfg, kernel, a, p);
 }
 
+template <int D>
+cudaError_t pick_columns(const SelectArgs& a, int sms, cudaStream_t st) {
+    if (a.group == 1) return run<D, 1>(a, sms, st);
+    if (a.group == 2) return run<D, 2>(a, sms, st);
+    if (a.group <= 4) return run<D, 4>(a, sms, st);
+    return run<D, 8>(a, sms, st);
+}
+
 }  // namespace
 
 cudaError_t launch_select(const SelectArgs& a, cudaStream_t st) {
@@ -419,9 +480,9 @@ cudaError_t launch_select(const SelectArgs& a, cudaStream_t st) {
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
-    if (a.c.d == 64) return run<64>(a, sms, st);
-    if (a.c.d == 128) return run<128>(a, sms, st);
-    return run<256>(a, sms, st);
+    if (a.c.d == 64) return pick_columns<64>(a, sms, st);
+    if (a.c.d == 128) return pick_columns<128>(a, sms, st);
+    return pick_columns<256>(a, sms, st);
 }
 
 }  // namespace kv
