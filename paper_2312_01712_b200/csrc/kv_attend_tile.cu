@@ -1,10 +1,20 @@
-// Attention of a prompt's tokens over listed blocks.
+// Attention of a prompt's tokens over listed blocks, on the tensor cores' own memory (tcgen05).
 //
 // Every (token, kv head) has a list of its own, but neighbouring tokens' lists are much alike.  A CTA takes a tile of consecutive
-// tokens of a request (up to 128 rows = token x query head) and one kv head, forms the union of their lists with one bit per token
-// and block, and walks it in ascending order: a block comes from L2 once per tile instead of once per token, and a warp computes
-// it only for those of its two groups of 8 rows that have a token that listed it.  Read once per token, 2048 tokens x 8
-// heads x 1024 keys are 8.6 GB from L2 for 69 GFLOP, which bound the kernel of kv_attend.cu on this work.
+// tokens of a request, 128 / group of them, so that its 128 rows are (token, query head) pairs of one kv head; it forms the union of their lists
+// with one bit per token and block and walks it in ascending order, 64 keys a step:
+//   S = Q K^T  (128 x 64, tcgen05.mma, fp32 in tensor memory), p = exp(S - m) for the rows that listed the block and see the key, 0 for the
+//   others, O += P V (128 x d, in tensor memory).
+// A block so comes from L2 once per tile instead of once per token, and the price is the products of rows that did not list it
+// (2048 tokens x 8 heads, 16 of 128 blocks each: unions of 27).  Three warps load keys and values (cp.async into 128-byte swizzled
+// tiles), one lane issues the products, four warps hold one row per thread for the softmax and put p over S in tensor memory; the product of the next step's keys is issued before
+// the previous step's values', so that it runs while the softmax does.  Two CTAs share an SM (d <= 128).  The running maximum moves only
+// when a logit exceeds it by more than 2^8, so that O is hardly ever read back to be scaled.
+//
+// A zero p must not meet an infinity or a not-a-number among the values of a block that the row did not list: the loading warps look
+// at every value, and a tile that holds such a one is done again row by row with plain arithmetic, each row over its own keys only.
+//
+// Every wait is bounded: one that runs out raises the status flag, all roles leave, and tensor memory is freed.
 #include <type_traits>
 
 #include "kv_mma.cuh"
@@ -13,53 +23,146 @@ namespace ivfpq {
 namespace kv {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
-constexpr int kRows = 16 * kWarps;       // columns of S^T: two groups of 8 per warp
-constexpr int kMaxTokens = 64;           // of a tile: bits of a block's mask
-constexpr int kKeys = 32;                // of a stage
+constexpr int kSoftWarps = 4, kLoadWarps = 3;
+constexpr int kThreads = 32 * (kSoftWarps + 1 + kLoadWarps);
+constexpr int kLoadThreads = 32 * kLoadWarps;
+constexpr int kRows = 128;
+constexpr int kKeys = 64;                // of a step
+constexpr int kStages = 2;
+constexpr unsigned kSpins = 1u << 22;
 
 template <int D>
 struct TileShape {
-    static constexpr int kStages = D == 256 ? 3 : 4;
-    static constexpr int kTileBytes = kKeys * D * 2;          // of keys, or of values
-    static constexpr int kRing = kStages * 2 * kTileBytes;
+    static constexpr int kSlabs = D / 64;                     // 128-byte wide slabs of a tile
+    static constexpr int kQ = kRows * D * 2, kKV = kKeys * D * 2;
+    static constexpr int kBytes = kQ + kStages * 2 * kKV;
+    static constexpr int kCols = D == 256 ? 512 : 256;        // of tensor memory: two S (P over the half of each), then O
+    static constexpr int kCtas = D == 256 ? 1 : 2;
 };
 
 struct TilePlan {
     int32_t tokens;          // of a tile
-    int32_t cols;            // columns of a token: its query heads rounded up to 1, 2, 4 or a multiple of 8
     int32_t list_cap;        // entries of the union
 };
 
+struct TileShared {
+    unsigned long long q_full, p_empty, drain;
+    unsigned long long p_full[2];        // one per S: a warp may be a step ahead of the others, and its arrival must not count for theirs
+    unsigned long long k_full[kStages], v_full[kStages], k_empty[kStages], v_empty[kStages], s_full[2];
+    uint32_t tmem;
+    volatile int abort;      // a wait ran out
+    volatile int special;    // a value is not finite
+    int count[kThreads / 32];
+};
+
+__device__ __forceinline__ bool wait_bar(unsigned long long* bar, uint32_t parity, TileShared* sh, int* status) {
+    const uint32_t at = smem_u32(bar);
+    for (unsigned i = 0; i < kSpins; ++i) {
+        if (mbar_try(at, parity)) return true;
+        if (sh->abort) return false;
+    }
+    sh->abort = 1;
+    atomicOr(status, kFlagWait);
+    return false;
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(unsigned long long* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0;\n"
+                 "  tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// The same with A in tensor memory: a row per lane, two 16-bit values per column.
+__device__ __forceinline__ void tc_mma_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0;\n"
+                 "  tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tc_load32(uint32_t at, uint32_t (&v)[32]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+                   "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
+                   "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]),
+                   "=r"(v[31])
+                 : "r"(at)
+                 : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tc_store32(uint32_t at, const uint32_t (&v)[32]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at),
+                 "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
+                 "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]),
+                 "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+                 : "memory");
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+// Descriptor of a 128-byte swizzled tile: groups of 8 rows of 128 bytes, 1024 bytes apart; `lead` is the distance of 64-element slabs where the
+// tile's rows run along the summed axis (values), unused otherwise.
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr, uint32_t lead) {
+    return (uint64_t)((addr >> 4) & 0x3fffu) | (uint64_t)((lead >> 4) & 0x3fffu) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+
 template <bool BF, int D>
-__global__ void __launch_bounds__(kThreads, 1) attend_tile_kernel(AttendArgs a, TilePlan p) {
+__global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_kernel(AttendArgs a, TilePlan p) {
     using S = TileShape<D>;
-    constexpr int KSTEPS = D / 16, MT = D / 16, CH = D / 8, NT = 2;
-    extern __shared__ __align__(128) char smem[];
-    unsigned long long* s_mask = reinterpret_cast<unsigned long long*>(smem + S::kRing);      // [max_blocks], then by entry
-    int2* s_list = reinterpret_cast<int2*>(s_mask + a.b.max_blocks);                           // [list_cap] (block, page)
-    __shared__ int s_count[kWarps];
-    __shared__ int s_total;
+    constexpr int CH = D / 8;
+    extern __shared__ __align__(1024) unsigned char dyn[];
+    const uint32_t pad = (1024u - (smem_u32(dyn) & 1023u)) & 1023u;
+    unsigned char* base = dyn + pad;
+    const uint32_t q_s = smem_u32(base), kv_s = q_s + S::kQ;                         // then stages of keys and values
+    TileShared* sh = reinterpret_cast<TileShared*>(base + S::kBytes);
+    unsigned long long* s_mask = reinterpret_cast<unsigned long long*>(sh + 1);        // [max_blocks], then by entry
+    int2* s_list = reinterpret_cast<int2*>(s_mask + a.b.max_blocks);                    // [list_cap] (block, page)
     const Cache& c = a.c;
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, lr = lane / 4, lc = lane % 4, head = blockIdx.y;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, head = blockIdx.y;
     int* status = reinterpret_cast<int*>(a.ws);
-    const uint32_t ring_u = smem_u32(smem);
 
     // ---- the tile's tokens: rows tok0 .. tok0 + n of request r, the first at position pos0 ----
-    int lo = 0, hi = a.b.nreq - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.b.start[mid] / p.tokens + mid <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
+    int r, n, tok0, pos0, nb;
+    {
+        int lo = 0, hi = a.b.nreq - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (a.b.start[mid] / p.tokens + mid <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
+        }
+        r = lo;
+        const int j0 = ((int)blockIdx.x - (a.b.start[r] / p.tokens + r)) * p.tokens;
+        const int2 mine = tokens_of(a.b, r, status);
+        if (j0 < 0 || j0 >= mine.y) return;
+        n = min(p.tokens, mine.y - j0);
+        tok0 = mine.x + j0;
+        pos0 = length_of(a.b, c, r, status) - mine.y + j0;
+        nb = (max(pos0 + n, 0) + c.page - 1) >> c.page_shift;
     }
-    const int r = lo;
-    const int j0 = ((int)blockIdx.x - (a.b.start[r] / p.tokens + r)) * p.tokens;
-    const int2 mine = tokens_of(a.b, r, status);
-    if (j0 < 0 || j0 >= mine.y) return;
-    const int n = min(p.tokens, mine.y - j0), tok0 = mine.x + j0;
-    const int pos0 = length_of(a.b, c, r, status) - mine.y + j0;
-    const int lim_hi = max(pos0 + n, 0);
-    const int nb = (lim_hi + c.page - 1) >> c.page_shift;
+    const int lim_hi = max(pos0 + n, 0), nrows = n * a.group;
+
+    if (tid == 0) {
+        mbar_init(smem_u32(&sh->q_full), kLoadThreads);
+        mbar_init(smem_u32(&sh->p_full[0]), 32 * kSoftWarps);
+        mbar_init(smem_u32(&sh->p_full[1]), 32 * kSoftWarps);
+        mbar_init(smem_u32(&sh->p_empty), 1);
+        mbar_init(smem_u32(&sh->drain), 1);
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(smem_u32(&sh->k_full[i]), kLoadThreads);
+            mbar_init(smem_u32(&sh->v_full[i]), kLoadThreads);
+            mbar_init(smem_u32(&sh->k_empty[i]), 1);
+            mbar_init(smem_u32(&sh->v_empty[i]), 1);
+        }
+        mbar_init(smem_u32(&sh->s_full[0]), 1);
+        mbar_init(smem_u32(&sh->s_full[1]), 1);
+        sh->abort = 0;
+        sh->special = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kSoftWarps) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem)), "r"(S::kCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
 
     // ---- union of the lists ----
     for (int i = tid; i < nb; i += kThreads) s_mask[i] = 0ull;
@@ -76,12 +179,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tile_kernel(AttendArgs a, 
         const unsigned long long m = i < nb ? s_mask[i] : 0ull;
         const int page = m ? page_of(a.b, c, r, i, status) : -1;
         const unsigned in = __ballot_sync(0xffffffffu, page >= 0);
-        if (lane == 0) s_count[warp] = __popc(in);
+        if (lane == 0) sh->count[warp] = __popc(in);
         __syncthreads();
         int at = total + __popc(in & ((1u << lane) - 1u));
-        for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) at += s_count[w];
-            total += s_count[w];
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w < warp) at += sh->count[w];
+            total += sh->count[w];
         }
         if (page >= 0) {
             s_list[at] = make_int2(i, page);
@@ -89,219 +192,288 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tile_kernel(AttendArgs a, 
         }
         __syncthreads();
     }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = sh->tmem;
 
-    // ---- queries and limits of the warp's columns ----
-    const int col0 = warp * 16;
-    uint32_t qf[NT][KSTEPS][2];
-    int lim[NT][2], bit[NT][2];
-    unsigned long long mine_mask[NT];
-    const float fscale = fmaxf(fabsf(a.scale), 1e-30f) * kLog2e;
-    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int col = col0 + nt * 8 + lr, j = col / p.cols, g = col % p.cols;
-        const bool real = j < n && g < a.group;
-        const char* qp = a.q.p + 2 * ((int64_t)(tok0 + (real ? j : 0)) * a.q.ts + (int64_t)(head * a.group + (real ? g : 0)) * a.q.hs);
-#pragma unroll
-        for (int s = 0; s < KSTEPS; ++s) {
-            qf[nt][s][0] = real ? *reinterpret_cast<const uint32_t*>(qp + 2 * (16 * s + 2 * lc)) ^ flip : 0u;
-            qf[nt][s][1] = real ? *reinterpret_cast<const uint32_t*>(qp + 2 * (16 * s + 8 + 2 * lc)) ^ flip : 0u;
-        }
-        mine_mask[nt] = 0ull;
-        for (int x = 0; x < 8; ++x) {
-            const int jj = (col0 + nt * 8 + x) / p.cols;
-            if (jj < n) mine_mask[nt] |= 1ull << jj;
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int jj = (col0 + nt * 8 + lc * 2 + x) / p.cols;
-            bit[nt][x] = min(jj, 63);
-            lim[nt][x] = jj < n ? max(pos0 + jj + 1, 0) : 0;
-        }
-    }
-    const int lim_lo = max(pos0 + min(col0 / p.cols, n - 1) + 1, 0);      // of the warp's first column
-    const bool packed = p.cols < 8;               // a group of 8 columns has several tokens
+    // a step: one entry (pages of 64), half of one (128), or two or four (32, 16)
+    const int piece = min(c.page, kKeys), pieces = kKeys / piece;                 // keys of an entry in a step, entries of a step
+    const int halves = c.page > kKeys ? c.page / kKeys : 1;
+    const int nstep = halves > 1 ? total * halves : (total + pieces - 1) / pieces;
 
-    float o[MT][NT][4], m[NT][2], l[NT][2];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) o[i][nt][x] = 0.f;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        m[nt][0] = m[nt][1] = -INFINITY;
-        l[nt][0] = l[nt][1] = 0.f;
-    }
-
-    // ---- stages: 32 keys (a page of 16: its 16) of an entry ----
-    const int per_shift = c.page_shift > 5 ? c.page_shift - 5 : 0;
-    const int nstage = total << per_shift, keys = min(c.page, kKeys);
-    auto issue = [&](int st) {
-        if (st < nstage) {
-            const int2 e = s_list[st >> per_shift];
-            const int off = (st & ((1 << per_shift) - 1)) * kKeys, pos = (e.x << c.page_shift) + off;
-            if (pos < lim_hi) {
-                const uint32_t dst = ring_u + (st % S::kStages) * 2 * S::kTileBytes;
-                const char* kp = c.k + 2 * (e.y * c.ks[0] + head * c.ks[1] + off * c.ks[2]);
-                const char* vp = c.v + 2 * (e.y * c.vs[0] + head * c.vs[1] + off * c.vs[2]);
-#pragma unroll
-                for (int i = 0; i < kKeys * CH / kThreads; ++i) {
-                    const int x = i * kThreads + tid, row = x / CH, ch = x % CH;
-                    const uint32_t at = row * (2 * D) + ((ch ^ (row & 7)) * 16);
-                    const bool real = row < keys && pos + row < lim_hi;
-                    const int rr = real ? row : 0;
-                    cp_async16(dst + at, kp + 2 * (rr * c.ks[2] + ch * 8), real);
-                    cp_async16(dst + S::kTileBytes + at, vp + 2 * (rr * c.vs[2] + ch * 8), real);
-                }
-            }
+    if (warp > kSoftWarps) {
+        // ---- loading warps ----
+        const int t = tid - 32 * (kSoftWarps + 1), ch = t % CH, row0 = t / CH;
+        constexpr int RS = kLoadThreads / CH;      // rows per pass
+        for (int row = row0; row < kRows; row += RS) {
+            const bool real = row < nrows;
+            const int j = real ? row / a.group : 0, g = real ? row % a.group : 0;
+            cp_async16(q_s + (ch / 8) * (kRows * 128) + row * 128 + (((ch & 7) ^ (row & 7)) * 16),
+                       a.q.p + 2 * ((int64_t)(tok0 + j) * a.q.ts + (int64_t)(head * a.group + g) * a.q.hs + ch * 8), real);
         }
         cp_async_commit();
-    };
-    for (int i = 0; i < S::kStages - 1; ++i) issue(i);
-    for (int st = 0; st < nstage; ++st) {
-        cp_async_wait<S::kStages - 2>();
-        __syncthreads();                          // the stage is here, and everybody is done with the one before
-        issue(st + S::kStages - 1);
-        const unsigned long long mask = s_mask[st >> per_shift];
-        const bool need0 = (mask & mine_mask[0]) != 0, need1 = (mask & mine_mask[1]) != 0;
-        const int pos = (s_list[st >> per_shift].x << c.page_shift) + (st & ((1 << per_shift) - 1)) * kKeys;
-        if (pos >= lim_hi || !(need0 || need1)) continue;
-        const uint32_t kt = ring_u + (st % S::kStages) * 2 * S::kTileBytes, vt = kt + S::kTileBytes;
-        const bool masked = packed || pos + kKeys > lim_lo || keys < kKeys;
-        auto work = [&](auto first, auto count) {
-            constexpr int N0 = decltype(first)::value, N1 = N0 + decltype(count)::value;
-            float s[2][NT][4];
-            {
-                const int row = (lane & 7) + ((lane >> 3) & 1) * 8, up = lane >> 4;
-#pragma unroll
-                for (int k = 0; k < KSTEPS; ++k)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint32_t f[4];
-                        ldmatrix4(f, kt + (i * 16 + row) * (2 * D) + (((2 * k + up) ^ (row & 7)) * 16));
-#pragma unroll
-                        for (int nt = N0; nt < N1; ++nt) {
-                            if (k == 0) mma16816_first<BF>(s[i][nt], f[0], f[1], f[2], f[3], qf[nt][k][0], qf[nt][k][1]);
-                            else mma16816<BF>(s[i][nt], f[0], f[1], f[2], f[3], qf[nt][k][0], qf[nt][k][1]);
-                        }
-                    }
-            }
-            if (masked) {
-#pragma unroll
-                for (int nt = N0; nt < N1; ++nt)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const bool listed = (mask >> bit[nt][x & 1]) & 1ull;
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int key = i * 16 + lr + (x >> 1) * 8;
-                            if (!listed || key >= keys || pos + key >= lim[nt][x & 1]) s[i][nt][x] = -INFINITY;
-                        }
-                    }
-            }
-            bool need = false;
-            float top[NT][2];
-#pragma unroll
-            for (int nt = N0; nt < N1; ++nt)
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    top[nt][x] = fmaxf(fmaxf(s[0][nt][x], s[0][nt][x + 2]), fmaxf(s[1][nt][x], s[1][nt][x + 2]));
-                    need |= fmaf(top[nt][x], fscale, -m[nt][x]) > kSlack;
-                }
-            if (__any_sync(0xffffffffu, need)) {
-#pragma unroll
-                for (int nt = N0; nt < N1; ++nt)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        float y = top[nt][x];
-#pragma unroll
-                        for (int k = 4; k < 32; k <<= 1) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, k));
-                        const float mn = fmaxf(m[nt][x], y * fscale);
-                        const float f = m[nt][x] == mn ? 1.f : ex2(m[nt][x] - mn);
-                        m[nt][x] = mn;
-                        l[nt][x] *= f;
-#pragma unroll
-                        for (int i = 0; i < MT; ++i) {
-                            o[i][nt][x] *= f;
-                            o[i][nt][x + 2] *= f;
-                        }
-                    }
-            }
-            uint32_t pf[2][NT][2];
-#pragma unroll
-            for (int nt = N0; nt < N1; ++nt) {
-                const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float e0 = ex2(fmaf(s[i][nt][0], fscale, -m0)), e1 = ex2(fmaf(s[i][nt][1], fscale, -m1));
-                    const float e2 = ex2(fmaf(s[i][nt][2], fscale, -m0)), e3 = ex2(fmaf(s[i][nt][3], fscale, -m1));
-                    l[nt][0] += e0 + e2;
-                    l[nt][1] += e1 + e3;
-                    pf[i][nt][0] = movmatrix(pack2<BF>(e0, e1));
-                    pf[i][nt][1] = movmatrix(pack2<BF>(e2, e3));
-                }
-            }
-            const int key = (lane & 7) + (lane >> 4) * 8, up = (lane >> 3) & 1;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    uint32_t f[4];
-                    ldmatrix4t(f, vt + (i * 16 + key) * (2 * D) + (((2 * mt + up) ^ (key & 7)) * 16));
-#pragma unroll
-                    for (int nt = N0; nt < N1; ++nt) mma16816<BF>(o[mt][nt], f[0], f[1], f[2], f[3], pf[i][nt][0], pf[i][nt][1]);
-                }
-        };
-        using I0 = std::integral_constant<int, 0>;
-        using I1 = std::integral_constant<int, 1>;
-        if (need0 && need1) work(I0{}, std::integral_constant<int, 2>{});
-        else if (need0) work(I0{}, I1{});
-        else work(I1{}, I1{});
-    }
-    cp_async_wait<0>();
-    __syncthreads();
+        cp_async_wait<0>();
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(smem_u32(&sh->q_full));
 
-    // ---- results through shared memory: [column][d] ----
-    char* so = smem + warp * 16 * (D + 8) * 2;
-    static_assert(kWarps * 16 * (D + 8) * 2 <= S::kRing, "the ring holds the rows");
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            float y = l[nt][x];
-#pragma unroll
-            for (int k = 4; k < 32; k <<= 1) y += __shfl_xor_sync(0xffffffffu, y, k);
-            const int cc = nt * 8 + lc * 2 + x, col = col0 + cc, j = col / p.cols, g = col % p.cols;
-            const bool nan = y != y;
-            const float inv = nan ? y : y > 0.f ? 1.f / y : 0.f;
-            if (a.lse && lr == 0 && j < n && g < a.group)
-                a.lse[(int64_t)(tok0 + j) * (c.nheads * a.group) + head * a.group + g] =
-                    nan ? y : y > 0.f ? (m[nt][x] + log2f(y)) * 0.6931471805599453f : -INFINITY;
-            uint16_t* at = reinterpret_cast<uint16_t*>(so) + cc * (D + 8) + lr;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                at[mt * 16] = to_bits(o[mt][nt][x] * inv, BF);
-                at[mt * 16 + 8] = to_bits(o[mt][nt][x + 2] * inv, BF);
+        const uint32_t off = (ch / 8) * (kKeys * 128);
+        constexpr uint32_t EXP = BF ? 0x7f807f80u : 0x7c007c00u, ONE = BF ? 0x00800080u : 0x04000400u;
+        uint32_t special = 0;
+        auto load = [&](int st, bool values) {
+            const uint32_t dst = kv_s + (st % kStages) * 2 * S::kKV + (values ? S::kKV : 0) + off;
+            const int64_t* str = values ? c.vs : c.ks;
+            const char* src0 = values ? c.v : c.k;
+            for (int row = row0; row < kKeys; row += RS) {
+                const int e = halves > 1 ? st / halves : st * pieces + row / piece;
+                const int in = halves > 1 ? (st % halves) * kKeys + row : row % piece;
+                const int2 en = e < total ? s_list[e] : make_int2(0, 0);
+                const bool real = e < total && (en.x << c.page_shift) + in < lim_hi;
+                cp_async16(dst + row * 128 + (((ch & 7) ^ (row & 7)) * 16),
+                           src0 + 2 * (en.y * str[0] + head * str[1] + (real ? in : 0) * str[2] + ch * 8), real);
+            }
+            cp_async_commit();
+        };
+        auto landed = [&](int st, bool values) {   // the thread's copies of that load are complete
+            if (values) {
+                const uint32_t at = kv_s + (st % kStages) * 2 * S::kKV + S::kKV + off;
+                for (int row = row0; row < kKeys; row += RS) {
+                    uint32_t x, y, z, w;
+                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x), "=r"(y), "=r"(z), "=r"(w) : "r"(at + row * 128 + (((ch & 7) ^ (row & 7)) * 16)) : "memory");
+                    special |= (((x & EXP) + ONE) | ((y & EXP) + ONE) | ((z & EXP) + ONE) | ((w & EXP) + ONE)) & 0x80008000u;
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            mbar_arrive(smem_u32(values ? &sh->v_full[st % kStages] : &sh->k_full[st % kStages]));
+        };
+        // Loads in the order K0 V0 K1 V1 ..., three under way.  What has landed is announced before the wait for a free slot: the slot of V(i + 2)
+        // is freed by a product that is issued after the one of K(i + 1).
+        bool ok = true;
+        for (int i = 0; i < 2 * nstep + 3 && ok; ++i) {
+            if (i >= 3) {
+                cp_async_wait<2>();
+                landed((i - 3) >> 1, (i - 3) & 1);
+            }
+            if (i < 2 * nstep) {
+                const int st = i >> 1;
+                const bool values = i & 1;
+                if (st >= kStages) ok = wait_bar(values ? &sh->v_empty[st % kStages] : &sh->k_empty[st % kStages], ((st / kStages) & 1) ^ 1, sh, status);
+                if (ok) load(st, values);
+            } else {
+                cp_async_commit();
             }
         }
-    __syncwarp();
-    for (int i = lane; i < 16 * CH; i += 32) {
-        const int cc = i / CH, ch = i % CH, col = col0 + cc, j = col / p.cols, g = col % p.cols;
-        if (j < n && g < a.group)
-            *reinterpret_cast<uint4*>(a.out + 2 * (((int64_t)(tok0 + j) * (c.nheads * a.group) + head * a.group + g) * D + ch * 8)) =
-                *reinterpret_cast<const uint4*>(so + (cc * (D + 8) + ch * 8) * 2);
+        cp_async_wait<0>();
+        if (special) sh->special = 1;
+    } else if (warp == kSoftWarps) {
+        if (lane == 0) {
+            // ---- products ----
+            constexpr uint32_t F = BF ? 1u : 0u;
+            constexpr uint32_t kS = 1u << 4 | F << 7 | F << 10 | (uint32_t)(kKeys >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
+            constexpr uint32_t kO = 1u << 4 | F << 7 | F << 10 | 1u << 16 | (uint32_t)(D >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
+            bool ok = nstep == 0 || wait_bar(&sh->q_full, 0, sh, status);
+            for (int st = 0; st <= nstep && ok && nstep > 0; ++st) {
+                if (st < nstep) {
+                    // S goes where P of two steps before was read
+                    if (st >= 2 && !(ok = wait_bar(&sh->p_empty, st & 1, sh, status))) break;
+                    ok = wait_bar(&sh->k_full[st % kStages], (st / kStages) & 1, sh, status);
+                    if (!ok) break;
+                    tc_after();
+                    const uint32_t k_at = kv_s + (st % kStages) * 2 * S::kKV;
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        tc_mma(tmem + (st & 1) * kKeys, tile_desc(q_s + (k / 4) * (kRows * 128) + (k % 4) * 32, 16),
+                               tile_desc(k_at + (k / 4) * (kKeys * 128) + (k % 4) * 32, 16), kS, k > 0);
+                    tc_commit(&sh->s_full[st & 1]);
+                    tc_commit(&sh->k_empty[st % kStages]);
+                }
+                if (st > 0) {
+                    const int pv = st - 1;
+                    ok = wait_bar(&sh->p_full[pv & 1], (pv >> 1) & 1, sh, status) && wait_bar(&sh->v_full[pv % kStages], (pv / kStages) & 1, sh, status);
+                    if (!ok) break;
+                    tc_after();
+                    const uint32_t v_at = kv_s + (pv % kStages) * 2 * S::kKV + S::kKV;
+#pragma unroll
+                    for (int k = 0; k < kKeys / 16; ++k)
+                        tc_mma_ta(tmem + 2 * kKeys, tmem + (pv & 1) * kKeys + k * 8, tile_desc(v_at + k * 2048, kKeys * 128), kO, pv > 0 || k > 0);
+                    tc_commit(&sh->v_empty[pv % kStages]);
+                    tc_commit(&sh->p_empty);
+                }
+            }
+            // nothing may be under way when tensor memory is freed
+            tc_commit(&sh->drain);
+            for (unsigned i = 0; i < kSpins; ++i)
+                if (mbar_try(smem_u32(&sh->drain), 0)) break;
+        }
+    } else {
+        // ---- softmax: one row per thread ----
+        const int row = warp * 32 + lane, j = min(row / a.group, n), lim = row < nrows ? max(pos0 + j + 1, 0) : 0;
+        const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+        const float fscale = fmaxf(fabsf(a.scale), 1e-30f) * kLog2e, sgn = a.scale < 0.f ? -fscale : fscale;
+        float m = -INFINITY, l = 0.f;
+        bool ok = true;
+        for (int st = 0; st < nstep && ok; ++st) {
+            // keys of the row in the step: `seen` bits
+            unsigned long long seen = 0ull;
+            if (row < nrows) {
+                if (halves > 1) {
+                    const int e = st / halves, v = min(max(lim - ((s_list[e].x << c.page_shift) + (st % halves) * kKeys), 0), kKeys);
+                    if (s_mask[e] >> j & 1ull) seen = v == kKeys ? ~0ull : (1ull << v) - 1ull;
+                } else {
+                    for (int i = 0; i < pieces; ++i) {
+                        const int e = st * pieces + i;
+                        if (e >= total || !(s_mask[e] >> j & 1ull)) continue;
+                        const int v = min(max(lim - (s_list[e].x << c.page_shift), 0), piece);
+                        seen |= (v == kKeys ? ~0ull : (1ull << v) - 1ull) << (i * piece);
+                    }
+                }
+            }
+            ok = wait_bar(&sh->s_full[st & 1], (st >> 1) & 1, sh, status);
+            if (!__all_sync(0xffffffffu, ok)) {
+                ok = false;
+                break;
+            }
+            tc_after();
+            uint32_t packed[32];
+            const bool none = !__any_sync(0xffffffffu, seen != 0ull);
+            float raise = 1.f;                     // factor of O and l
+            if (none) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) packed[i] = 0u;
+            } else {
+                const bool partly = __any_sync(0xffffffffu, seen != 0ull && ~seen != 0ull);
+                uint32_t v[2][32];
+                tc_load32(lanes + (st & 1) * kKeys, v[0]);
+                tc_load32(lanes + (st & 1) * kKeys + 32, v[1]);
+                float top = -INFINITY;
+                if (partly) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!((h ? (uint32_t)(seen >> 32) : (uint32_t)seen) >> i & 1u)) v[h][i] = __float_as_uint(sgn < 0.f ? INFINITY : -INFINITY);
+                }
+                if (sgn < 0.f) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[h][i] ^= 0x80000000u;
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v[h][i]));
+                top = seen ? top * fscale : -INFINITY;
+                if (top > m + kSlack) {
+                    if (m != -INFINITY) raise = ex2(m - top);      // else the row's first keys: nothing was summed
+                    m = top;
+                    l *= raise;
+                }
+                const float mm = m == -INFINITY ? 0.f : m;
+                float sum = 0.f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        const float e0 = ex2(fmaf(__uint_as_float(v[h][i]), fscale, -mm)), e1 = ex2(fmaf(__uint_as_float(v[h][i + 1]), fscale, -mm));
+                        sum += e0 + e1;
+                        packed[h * 16 + i / 2] = pack2<BF>(e0, e1);
+                    }
+                if (seen) {
+                    l += sum;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) packed[i] = 0u;
+                }
+            }
+            if (st > 0 && __any_sync(0xffffffffu, raise != 1.f)) {
+                // the previous step has written O; the one before it had when S of this step was issued, so the parity is of that step
+                ok = __all_sync(0xffffffffu, wait_bar(&sh->p_empty, (st - 1) & 1, sh, status));
+                if (!ok) break;
+                tc_after();
+                for (int cc = 0; cc < D; cc += 32) {
+                    uint32_t x[32];
+                    tc_load32(lanes + 2 * kKeys + cc, x);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * raise);
+                    tc_store32(lanes + 2 * kKeys + cc, x);
+                }
+            }
+            tc_store32(lanes + (st & 1) * kKeys, packed);
+            tc_before();
+            mbar_arrive(smem_u32(&sh->p_full[st & 1]));
+        }
+        if (ok && nstep > 0) ok = wait_bar(&sh->drain, 0, sh, status);      // all products are done
+        ok = __all_sync(0xffffffffu, ok);
+        tc_after();
+        // ---- results: a row is 2 D contiguous bytes of its thread ----
+        const bool nan = l != l;
+        const float inv = nan ? l : l > 0.f ? 1.f / l : 0.f;
+        const int64_t orow = (int64_t)(tok0 + row / a.group) * (c.nheads * a.group) + head * a.group + row % a.group;
+        for (int cc = 0; cc < D; cc += 32) {
+            uint32_t x[32];
+            if (nstep > 0) tc_load32(lanes + 2 * kKeys + cc, x);
+            if (row < nrows) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    float y[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] = nstep > 0 && l != 0.f ? __uint_as_float(x[i + k]) * inv : 0.f;
+                    *reinterpret_cast<uint4*>(a.out + 2 * (orow * D + cc + i)) = pack8(y, BF);
+                }
+            }
+        }
+        if (a.lse && row < nrows) a.lse[orow] = nan ? l : l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        tc_before();
+    }
+    __syncthreads();
+    if (warp == kSoftWarps) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kCols) : "memory");
+    }
+    if (sh->special && !sh->abort) {
+        // ---- a value is not finite: every row over its own keys, a warp per row ----
+        constexpr int E = D / 32;
+        for (int row = warp; row < nrows; row += kThreads / 32) {
+            const int j = row / a.group, h = head * a.group + row % a.group, lim = pos0 + j + 1, e0 = lane * E;
+            float q[E], o[E], m = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                q[i] = to_float(reinterpret_cast<const uint16_t*>(a.q.p + 2 * ((int64_t)(tok0 + j) * a.q.ts + (int64_t)h * a.q.hs))[e0 + i], BF) * a.scale * kLog2e;
+                o[i] = 0.f;
+            }
+            for (int e = 0; e < total; ++e) {
+                if (!(s_mask[e] >> j & 1ull)) continue;
+                const int2 en = s_list[e];
+                const int end = min(c.page, lim - (en.x << c.page_shift));
+                for (int t = 0; t < end; ++t) {
+                    const uint16_t* kp = reinterpret_cast<const uint16_t*>(c.k) + en.y * c.ks[0] + head * c.ks[1] + t * c.ks[2] + e0;
+                    const uint16_t* vp = reinterpret_cast<const uint16_t*>(c.v) + en.y * c.vs[0] + head * c.vs[1] + t * c.vs[2] + e0;
+                    float x = 0.f;
+#pragma unroll
+                    for (int i = 0; i < E; ++i) x = fmaf(q[i], to_float(kp[i], BF), x);
+#pragma unroll
+                    for (int s = 16; s; s >>= 1) x += __shfl_xor_sync(0xffffffffu, x, s);
+                    const float mn = fmaxf(m, x), f = m == mn ? 1.f : ex2(m - mn), pr = ex2(x - mn);
+                    m = mn;
+                    l = fmaf(l, f, pr);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) o[i] = fmaf(pr, to_float(vp[i], BF), o[i] * f);
+                }
+            }
+            const int64_t orow = (int64_t)(tok0 + j) * (c.nheads * a.group) + h;
+#pragma unroll
+            for (int i = 0; i < E; ++i) reinterpret_cast<uint16_t*>(a.out)[orow * D + e0 + i] = to_bits(l == 0.f ? 0.f : o[i] / l, BF);
+        }
     }
 }
 
 template <int D>
 size_t tile_smem(const AttendArgs& a, TilePlan* p) {
-    p->cols = a.group <= 2 ? a.group : a.group <= 4 ? 4 : (a.group + 7) / 8 * 8;
-    p->tokens = kRows / p->cols < kMaxTokens ? kRows / p->cols : kMaxTokens;
+    p->tokens = kRows / a.group < 64 ? kRows / a.group : 64;      // a block's mask has 64 bits
     const int64_t entries = (int64_t)p->tokens * a.nselect;
     p->list_cap = (int32_t)(entries < a.b.max_blocks ? entries : a.b.max_blocks);
-    return (size_t)TileShape<D>::kRing + (size_t)a.b.max_blocks * 8 + (size_t)p->list_cap * 8;
+    return 1024 + (size_t)TileShape<D>::kBytes + sizeof(TileShared) + (size_t)a.b.max_blocks * 8 + (size_t)p->list_cap * 8;
 }
 
 template <bool BF, int D>
@@ -317,7 +489,7 @@ cudaError_t run(const AttendArgs& a, cudaStream_t st) {
 
 }  // namespace
 
-// Tiles pay where tokens of a request share lists: several tokens a request, and masks that fit beside the ring.
+// Tiles pay where tokens of a request share lists: several tokens a request, and masks that fit beside the tiles.
 bool attend_tile_serves(const AttendArgs& a) {
     if (!a.blocks || !a.b.start || a.c.format == IVFPQ_KV_INT4 || a.b.ntok < 8 * (int64_t)a.b.nreq) return false;
     TilePlan p{};
