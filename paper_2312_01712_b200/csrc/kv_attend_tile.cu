@@ -200,6 +200,7 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
     // a step: one entry (pages of 64), half of one (128), or two or four (32, 16)
     const int piece = min(c.page, kKeys), pieces = kKeys / piece;                 // keys of an entry in a step, entries of a step
     const int halves = c.page > kKeys ? c.page / kKeys : 1;
+    const int half_shift = halves > 1 ? 1 : 0;
     const int nstep = halves > 1 ? total * halves : (total + pieces - 1) / pieces;
 
     if (warp > kSoftWarps) {
@@ -222,21 +223,33 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
         uint32_t special = 0;
         auto load = [&](int st, bool values) {
             const uint32_t dst = kv_s + (st % kStages) * 2 * S::kKV + (values ? S::kKV : 0) + off;
-            const int64_t* str = values ? c.vs : c.ks;
-            const char* src0 = values ? c.v : c.k;
-            for (int row = row0; row < kKeys; row += RS) {
-                const int e = halves > 1 ? st / halves : st * pieces + row / piece;
-                const int in = halves > 1 ? (st % halves) * kKeys + row : row % piece;
-                const int2 en = e < total ? s_list[e] : make_int2(0, 0);
-                const bool real = e < total && (en.x << c.page_shift) + in < lim_hi;
-                cp_async16(dst + row * 128 + (((ch & 7) ^ (row & 7)) * 16),
-                           src0 + 2 * (en.y * str[0] + head * str[1] + (real ? in : 0) * str[2] + ch * 8), real);
+            const int64_t s0 = values ? c.vs[0] : c.ks[0], s1 = values ? c.vs[1] : c.ks[1], s2 = values ? c.vs[2] : c.ks[2];
+            const char* src0 = (values ? c.v : c.k) + 2 * (head * s1 + ch * 8);
+            if (pieces == 1) {
+                // one entry: rows a fixed distance apart
+                const int2 en = s_list[st >> half_shift];
+                const int in = (st & (halves - 1)) * kKeys, left = lim_hi - (en.x << c.page_shift) - in;      // rows that are held
+                const char* src = src0 + 2 * (en.y * s0 + (in + row0) * s2);
+#pragma unroll
+                for (int i = 0; i < (kKeys + RS - 1) / RS; ++i) {
+                    const int row = row0 + i * RS;
+                    if (row < kKeys) cp_async16(dst + row * 128 + (((ch & 7) ^ (row & 7)) * 16), row < left ? src : src0, row < left);
+                    src += 2 * RS * s2;
+                }
+            } else {
+                for (int row = row0; row < kKeys; row += RS) {
+                    const int e = st * pieces + (row >> c.page_shift), in = row & (piece - 1);
+                    const int2 en = e < total ? s_list[e] : make_int2(0, 0);
+                    const bool real = e < total && (en.x << c.page_shift) + in < lim_hi;
+                    cp_async16(dst + row * 128 + (((ch & 7) ^ (row & 7)) * 16), src0 + 2 * (en.y * s0 + (real ? in : 0) * s2), real);
+                }
             }
             cp_async_commit();
         };
         auto landed = [&](int st, bool values) {   // the thread's copies of that load are complete
             if (values) {
                 const uint32_t at = kv_s + (st % kStages) * 2 * S::kKV + S::kKV + off;
+#pragma unroll 4
                 for (int row = row0; row < kKeys; row += RS) {
                     uint32_t x, y, z, w;
                     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x), "=r"(y), "=r"(z), "=r"(w) : "r"(at + row * 128 + (((ch & 7) ^ (row & 7)) * 16)) : "memory");
@@ -316,15 +329,15 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
             // keys of the row in the step: `seen` bits
             unsigned long long seen = 0ull;
             if (row < nrows) {
-                if (halves > 1) {
-                    const int e = st / halves, v = min(max(lim - ((s_list[e].x << c.page_shift) + (st % halves) * kKeys), 0), kKeys);
+                if (pieces == 1) {
+                    const int e = st >> half_shift, v = min(max(lim - ((s_list[e].x << c.page_shift) + (st & (halves - 1)) * kKeys), 0), kKeys);
                     if (s_mask[e] >> j & 1ull) seen = v == kKeys ? ~0ull : (1ull << v) - 1ull;
                 } else {
                     for (int i = 0; i < pieces; ++i) {
                         const int e = st * pieces + i;
                         if (e >= total || !(s_mask[e] >> j & 1ull)) continue;
                         const int v = min(max(lim - (s_list[e].x << c.page_shift), 0), piece);
-                        seen |= (v == kKeys ? ~0ull : (1ull << v) - 1ull) << (i * piece);
+                        seen |= ((1ull << v) - 1ull) << (i * piece);
                     }
                 }
             }
