@@ -23,9 +23,8 @@ namespace ivfpq {
 namespace kv {
 namespace {
 
-constexpr int kSoftWarps = 4, kLoadWarps = 3;
-constexpr int kThreads = 32 * (kSoftWarps + 1 + kLoadWarps);
-constexpr int kLoadThreads = 32 * kLoadWarps;
+constexpr int kSoftWarps = 4, kKeyWarps = 1, kValueWarps = 2;      // and one that issues the products
+constexpr int kThreads = 32 * (kSoftWarps + 1 + kKeyWarps + kValueWarps);
 constexpr int kRows = 128;
 constexpr int kKeys = 64;                // of a step
 constexpr int kStages = 2;
@@ -33,7 +32,6 @@ constexpr unsigned kSpins = 1u << 22;
 
 template <int D>
 struct TileShape {
-    static constexpr int kSlabs = D / 64;                     // 128-byte wide slabs of a tile
     static constexpr int kQ = kRows * D * 2, kKV = kKeys * D * 2;
     static constexpr int kBytes = kQ + kStages * 2 * kKV;
     static constexpr int kCols = D == 256 ? 512 : 256;        // of tensor memory: two S (P over the half of each), then O
@@ -142,14 +140,14 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
     const int lim_hi = max(pos0 + n, 0), nrows = n * a.group;
 
     if (tid == 0) {
-        mbar_init(smem_u32(&sh->q_full), kLoadThreads);
+        mbar_init(smem_u32(&sh->q_full), 32 * kValueWarps);
         mbar_init(smem_u32(&sh->p_full[0]), 32 * kSoftWarps);
         mbar_init(smem_u32(&sh->p_full[1]), 32 * kSoftWarps);
         mbar_init(smem_u32(&sh->p_empty), 1);
         mbar_init(smem_u32(&sh->drain), 1);
         for (int i = 0; i < kStages; ++i) {
-            mbar_init(smem_u32(&sh->k_full[i]), kLoadThreads);
-            mbar_init(smem_u32(&sh->v_full[i]), kLoadThreads);
+            mbar_init(smem_u32(&sh->k_full[i]), 32 * kKeyWarps);
+            mbar_init(smem_u32(&sh->v_full[i]), 32 * kValueWarps);
             mbar_init(smem_u32(&sh->k_empty[i]), 1);
             mbar_init(smem_u32(&sh->v_empty[i]), 1);
         }
@@ -204,80 +202,70 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
     const int nstep = halves > 1 ? total * halves : (total + pieces - 1) / pieces;
 
     if (warp > kSoftWarps) {
-        // ---- loading warps ----
-        const int t = tid - 32 * (kSoftWarps + 1), ch = t % CH, row0 = t / CH;
-        constexpr int RS = kLoadThreads / CH;      // rows per pass
-        for (int row = row0; row < kRows; row += RS) {
-            const bool real = row < nrows;
-            const int j = real ? row / a.group : 0, g = real ? row % a.group : 0;
-            cp_async16(q_s + (ch / 8) * (kRows * 128) + row * 128 + (((ch & 7) ^ (row & 7)) * 16),
-                       a.q.p + 2 * ((int64_t)(tok0 + j) * a.q.ts + (int64_t)(head * a.group + g) * a.q.hs + ch * 8), real);
-        }
-        cp_async_commit();
-        cp_async_wait<0>();
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        mbar_arrive(smem_u32(&sh->q_full));
-
-        const uint32_t off = (ch / 8) * (kKeys * 128);
-        constexpr uint32_t EXP = BF ? 0x7f807f80u : 0x7c007c00u, ONE = BF ? 0x00800080u : 0x04000400u;
-        uint32_t special = 0;
-        auto load = [&](int st, bool values) {
-            const uint32_t dst = kv_s + (st % kStages) * 2 * S::kKV + (values ? S::kKV : 0) + off;
-            const int64_t s0 = values ? c.vs[0] : c.ks[0], s1 = values ? c.vs[1] : c.ks[1], s2 = values ? c.vs[2] : c.ks[2];
-            const char* src0 = (values ? c.v : c.k) + 2 * (head * s1 + ch * 8);
-            if (pieces == 1) {
-                // one entry: rows a fixed distance apart
-                const int2 en = s_list[st >> half_shift];
-                const int in = (st & (halves - 1)) * kKeys, left = lim_hi - (en.x << c.page_shift) - in;      // rows that are held
-                const char* src = src0 + 2 * (en.y * s0 + (in + row0) * s2);
-#pragma unroll
-                for (int i = 0; i < (kKeys + RS - 1) / RS; ++i) {
-                    const int row = row0 + i * RS;
-                    if (row < kKeys) cp_async16(dst + row * 128 + (((ch & 7) ^ (row & 7)) * 16), row < left ? src : src0, row < left);
-                    src += 2 * RS * s2;
+        // ---- loading warps: one for the keys, two for the values (and the queries before them); each announces a tile as soon as it is
+        //      there, and then waits for a free slot ----
+        const bool values = warp > kSoftWarps + kKeyWarps;
+        auto run = [&](auto which) {
+            constexpr bool V = decltype(which)::value;
+            constexpr int N = 32 * (V ? kValueWarps : kKeyWarps), RS = N / CH > 0 ? N / CH : 1;      // threads; rows per pass
+            constexpr uint32_t EXP = BF ? 0x7f807f80u : 0x7c007c00u, ONE = BF ? 0x00800080u : 0x04000400u;
+            const int t = tid - 32 * (kSoftWarps + 1 + (V ? kKeyWarps : 0)), ch = t % CH, row0 = t / CH;
+            if (V) {
+                for (int row = row0; row < kRows; row += RS) {
+                    const bool real = row < nrows;
+                    const int j = real ? row / a.group : 0, g = real ? row % a.group : 0;
+                    cp_async16(q_s + (ch / 8) * (kRows * 128) + row * 128 + (((ch & 7) ^ (row & 7)) * 16),
+                               a.q.p + 2 * ((int64_t)(tok0 + j) * a.q.ts + (int64_t)(head * a.group + g) * a.q.hs + ch * 8), real);
                 }
-            } else {
-                for (int row = row0; row < kKeys; row += RS) {
-                    const int e = st * pieces + (row >> c.page_shift), in = row & (piece - 1);
-                    const int2 en = e < total ? s_list[e] : make_int2(0, 0);
-                    const bool real = e < total && (en.x << c.page_shift) + in < lim_hi;
-                    cp_async16(dst + row * 128 + (((ch & 7) ^ (row & 7)) * 16), src0 + 2 * (en.y * s0 + (real ? in : 0) * s2), real);
-                }
-            }
-            cp_async_commit();
-        };
-        auto landed = [&](int st, bool values) {   // the thread's copies of that load are complete
-            if (values) {
-                const uint32_t at = kv_s + (st % kStages) * 2 * S::kKV + S::kKV + off;
-#pragma unroll 4
-                for (int row = row0; row < kKeys; row += RS) {
-                    uint32_t x, y, z, w;
-                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x), "=r"(y), "=r"(z), "=r"(w) : "r"(at + row * 128 + (((ch & 7) ^ (row & 7)) * 16)) : "memory");
-                    special |= (((x & EXP) + ONE) | ((y & EXP) + ONE) | ((z & EXP) + ONE) | ((w & EXP) + ONE)) & 0x80008000u;
-                }
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            mbar_arrive(smem_u32(values ? &sh->v_full[st % kStages] : &sh->k_full[st % kStages]));
-        };
-        // Loads in the order K0 V0 K1 V1 ..., three under way.  What has landed is announced before the wait for a free slot: the slot of V(i + 2)
-        // is freed by a product that is issued after the one of K(i + 1).
-        bool ok = true;
-        for (int i = 0; i < 2 * nstep + 3 && ok; ++i) {
-            if (i >= 3) {
-                cp_async_wait<2>();
-                landed((i - 3) >> 1, (i - 3) & 1);
-            }
-            if (i < 2 * nstep) {
-                const int st = i >> 1;
-                const bool values = i & 1;
-                if (st >= kStages) ok = wait_bar(values ? &sh->v_empty[st % kStages] : &sh->k_empty[st % kStages], ((st / kStages) & 1) ^ 1, sh, status);
-                if (ok) load(st, values);
-            } else {
                 cp_async_commit();
+                cp_async_wait<0>();
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                mbar_arrive(smem_u32(&sh->q_full));
             }
-        }
-        cp_async_wait<0>();
-        if (special) sh->special = 1;
+            const int64_t s0 = V ? c.vs[0] : c.ks[0], s1 = V ? c.vs[1] : c.ks[1], s2 = V ? c.vs[2] : c.ks[2];
+            const char* src0 = (V ? c.v : c.k) + 2 * (head * s1 + ch * 8);
+            uint32_t special = 0;
+            for (int st = 0; st < nstep; ++st) {
+                const int slot = st % kStages;
+                if (st >= kStages && !wait_bar(V ? &sh->v_empty[slot] : &sh->k_empty[slot], ((st / kStages) & 1) ^ 1, sh, status)) break;
+                const uint32_t dst = kv_s + slot * 2 * S::kKV + (V ? S::kKV : 0) + (ch / 8) * (kKeys * 128);
+                if (pieces == 1) {
+                    // one entry: rows a fixed distance apart
+                    const int2 en = s_list[st >> half_shift];
+                    const int in = (st & (halves - 1)) * kKeys, left = lim_hi - (en.x << c.page_shift) - in;      // rows that are held
+                    const char* src = src0 + 2 * (en.y * s0 + (in + row0) * s2);
+#pragma unroll 8
+                    for (int row = row0; row < kKeys; row += RS) {
+                        cp_async16(dst + row * 128 + (((ch & 7) ^ (row & 7)) * 16), row < left ? src : src0, row < left);
+                        src += 2 * RS * s2;
+                    }
+                } else {
+                    for (int row = row0; row < kKeys; row += RS) {
+                        const int e = st * pieces + (row >> c.page_shift), in = row & (piece - 1);
+                        const int2 en = e < total ? s_list[e] : make_int2(0, 0);
+                        const bool real = e < total && (en.x << c.page_shift) + in < lim_hi;
+                        cp_async16(dst + row * 128 + (((ch & 7) ^ (row & 7)) * 16), src0 + 2 * (en.y * s0 + (real ? in : 0) * s2), real);
+                    }
+                }
+                cp_async_commit();
+                cp_async_wait<0>();
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                mbar_arrive(smem_u32(V ? &sh->v_full[slot] : &sh->k_full[slot]));
+                if (V) {
+                    // the product only reads the tile, so it may be looked at meanwhile; the slot is written again by these threads
+#pragma unroll 8
+                    for (int row = row0; row < kKeys; row += RS) {
+                        uint32_t x, y, z, w;
+                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x), "=r"(y), "=r"(z), "=r"(w) : "r"(dst + row * 128 + (((ch & 7) ^ (row & 7)) * 16)) : "memory");
+                        special |= (((x & EXP) + ONE) | ((y & EXP) + ONE) | ((z & EXP) + ONE) | ((w & EXP) + ONE)) & 0x80008000u;
+                    }
+                }
+            }
+            cp_async_wait<0>();
+            if (special) sh->special = 1;
+        };
+        if (values) run(std::true_type{});
+        else run(std::false_type{});
     } else if (warp == kSoftWarps) {
         if (lane == 0) {
             // ---- products ----
