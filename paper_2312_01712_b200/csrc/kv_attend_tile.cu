@@ -28,7 +28,7 @@ constexpr int kThreads = 32 * (kSoftWarps + 1 + kKeyWarps + kValueWarps);
 constexpr int kRows = 128;
 constexpr int kKeys = 64;                // of a step
 constexpr int kStages = 2;
-constexpr unsigned kSpins = 1u << 22;
+constexpr unsigned kSpins = 1u << 22;        // tries of a wait
 
 template <int D>
 struct TileShape {
@@ -53,10 +53,13 @@ struct TileShared {
     int count[kThreads / 32];
 };
 
+// RELAXED: the waiting warps are ahead of the others and sleep between tries, which leaves the issue slots to the softmax.
+template <bool RELAXED = false>
 __device__ __forceinline__ bool wait_bar(unsigned long long* bar, uint32_t parity, TileShared* sh, int* status) {
     const uint32_t at = smem_u32(bar);
     for (unsigned i = 0; i < kSpins; ++i) {
         if (mbar_try(at, parity)) return true;
+        if (RELAXED) __nanosleep(200);
         if (sh->abort) return false;
     }
     sh->abort = 1;
@@ -227,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
             uint32_t special = 0;
             for (int st = 0; st < nstep; ++st) {
                 const int slot = st % kStages;
-                if (st >= kStages && !wait_bar(V ? &sh->v_empty[slot] : &sh->k_empty[slot], ((st / kStages) & 1) ^ 1, sh, status)) break;
+                if (st >= kStages && !wait_bar<true>(V ? &sh->v_empty[slot] : &sh->k_empty[slot], ((st / kStages) & 1) ^ 1, sh, status)) break;
                 const uint32_t dst = kv_s + slot * 2 * S::kKV + (V ? S::kKV : 0) + (ch / 8) * (kKeys * 128);
                 if (pieces == 1) {
                     // one entry: rows a fixed distance apart
@@ -310,7 +313,7 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
         // ---- softmax: one row per thread ----
         const int row = warp * 32 + lane, j = min(row / a.group, n), lim = row < nrows ? max(pos0 + j + 1, 0) : 0;
         const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
-        const float fscale = fmaxf(fabsf(a.scale), 1e-30f) * kLog2e, sgn = a.scale < 0.f ? -fscale : fscale;
+        const float fscale = fmaxf(a.scale, 1e-30f) * kLog2e;      // a masked product is -infinity and has to stay it
         float m = -INFINITY, l = 0.f;
         bool ok = true;
         for (int st = 0; st < nstep && ok; ++st) {
@@ -346,24 +349,19 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
                 uint32_t v[2][32];
                 tc_load32(lanes + (st & 1) * kKeys, v[0]);
                 tc_load32(lanes + (st & 1) * kKeys + 32, v[1]);
-                float top = -INFINITY;
                 if (partly) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (!((h ? (uint32_t)(seen >> 32) : (uint32_t)seen) >> i & 1u)) v[h][i] = __float_as_uint(sgn < 0.f ? INFINITY : -INFINITY);
+                            if (!((h ? (uint32_t)(seen >> 32) : (uint32_t)seen) >> i & 1u)) v[h][i] = 0xff800000u;      // -infinity
                 }
-                if (sgn < 0.f) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[h][i] ^= 0x80000000u;
-                }
+                float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v[h][i]));
+                    for (int i = 0; i < 32; i += 2) t4[i / 2 % 4] = fmaxf(t4[i / 2 % 4], fmaxf(__uint_as_float(v[h][i]), __uint_as_float(v[h][i + 1])));
+                float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
                 top = seen ? top * fscale : -INFINITY;
                 if (top > m + kSlack) {
                     if (m != -INFINITY) raise = ex2(m - top);      // else the row's first keys: nothing was summed
@@ -371,17 +369,17 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
                     l *= raise;
                 }
                 const float mm = m == -INFINITY ? 0.f : m;
-                float sum = 0.f;
+                float sum4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
                         const float e0 = ex2(fmaf(__uint_as_float(v[h][i]), fscale, -mm)), e1 = ex2(fmaf(__uint_as_float(v[h][i + 1]), fscale, -mm));
-                        sum += e0 + e1;
+                        sum4[i / 2 % 4] += e0 + e1;
                         packed[h * 16 + i / 2] = pack2<BF>(e0, e1);
                     }
                 if (seen) {
-                    l += sum;
+                    l += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) packed[i] = 0u;
@@ -492,7 +490,7 @@ cudaError_t run(const AttendArgs& a, cudaStream_t st) {
 
 // Tiles pay where tokens of a request share lists: several tokens a request, and masks that fit beside the tiles.
 bool attend_tile_serves(const AttendArgs& a) {
-    if (!a.blocks || !a.b.start || a.c.format == IVFPQ_KV_INT4 || a.b.ntok < 8 * (int64_t)a.b.nreq) return false;
+    if (!a.blocks || !a.b.start || a.c.format == IVFPQ_KV_INT4 || a.scale < 0.f || a.b.ntok < 8 * (int64_t)a.b.nreq) return false;
     TilePlan p{};
     const size_t smem = a.c.d == 64 ? tile_smem<64>(a, &p) : a.c.d == 128 ? tile_smem<128>(a, &p) : tile_smem<256>(a, &p);
     return smem <= 220 * 1024;
