@@ -7,7 +7,7 @@
 //   others, O += P V (128 x d, in tensor memory).
 // A block so comes from L2 once per tile instead of once per token, and the price is the products of rows that did not list it
 // (2048 tokens x 8 heads, 16 of 128 blocks each: unions of 27).  Three warps load keys and values (cp.async into 128-byte swizzled
-// tiles), one lane issues the products, four warps hold one row per thread for the softmax and put p over S in tensor memory; the product of the next step's keys is issued before
+// tiles), one issues the products, four warps hold one row per thread for the softmax and put p over S in tensor memory; the product of the next step's keys is issued before
 // the previous step's values', so that it runs while the softmax does.  Two CTAs share an SM (d <= 128).  The running maximum moves only
 // when a logit exceeds it by more than 2^8, so that O is hardly ever read back to be scaled.
 //
@@ -27,7 +27,7 @@ constexpr int kSoftWarps = 4, kKeyWarps = 1, kValueWarps = 2;      // and one th
 constexpr int kThreads = 32 * (kSoftWarps + 1 + kKeyWarps + kValueWarps);
 constexpr int kRows = 128;
 constexpr int kKeys = 64;                // of a step
-constexpr int kStages = 2;
+constexpr int kStages = 2;               // of keys and of values: the products' code counts on two
 constexpr unsigned kSpins = 1u << 22;        // tries of a wait
 
 template <int D>
@@ -101,6 +101,11 @@ __device__ __forceinline__ void tc_store32(uint32_t at, const uint32_t (&v)[32])
                  "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
                  : "memory");
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(p));
+    return p;
 }
 // Descriptor of a 128-byte swizzled tile: groups of 8 rows of 128 bytes, 1024 bytes apart; `lead` is the distance of 64-element slabs where the
 // tile's rows run along the summed axis (values), unused otherwise.
@@ -270,45 +275,58 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
         if (values) run(std::true_type{});
         else run(std::false_type{});
     } else if (warp == kSoftWarps) {
-        if (lane == 0) {
-            // ---- products ----
-            constexpr uint32_t F = BF ? 1u : 0u;
-            constexpr uint32_t kS = 1u << 4 | F << 7 | F << 10 | (uint32_t)(kKeys >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
-            constexpr uint32_t kO = 1u << 4 | F << 7 | F << 10 | 1u << 16 | (uint32_t)(D >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
-            bool ok = nstep == 0 || wait_bar(&sh->q_full, 0, sh, status);
-            for (int st = 0; st <= nstep && ok && nstep > 0; ++st) {
-                if (st < nstep) {
-                    // S goes where P of two steps before was read
-                    if (st >= 2 && !(ok = wait_bar(&sh->p_empty, st & 1, sh, status))) break;
-                    ok = wait_bar(&sh->k_full[st % kStages], (st / kStages) & 1, sh, status);
-                    if (!ok) break;
-                    tc_after();
-                    const uint32_t k_at = kv_s + (st % kStages) * 2 * S::kKV;
+        // ---- products: the warp runs as one, so that descriptors stay in uniform registers, and one lane issues ----
+        constexpr uint32_t F = BF ? 1u : 0u;
+        constexpr uint32_t kS = 1u << 4 | F << 7 | F << 10 | (uint32_t)(kKeys >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
+        constexpr uint32_t kO = 1u << 4 | F << 7 | F << 10 | 1u << 16 | (uint32_t)(D >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
+        const uint32_t kv_u = __shfl_sync(0xffffffffu, kv_s, 0), tm = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint64_t q_desc = tile_desc(__shfl_sync(0xffffffffu, q_s, 0), 16);
+        const uint64_t k_desc = tile_desc(kv_u, 16), v_desc = tile_desc(kv_u + S::kKV, kKeys * 128);
+        constexpr uint64_t kStage = 2 * S::kKV >> 4;               // descriptors count in 16 bytes
+        bool ok = nstep == 0 || wait_bar(&sh->q_full, 0, sh, status);
+        for (int st = 0; st <= nstep && ok && nstep > 0; ++st) {
+            if (st < nstep) {
+                // S goes where P of two steps before was read
+                if (st >= 2) ok = wait_bar(&sh->p_empty, st & 1, sh, status);
+                ok = ok && wait_bar(&sh->k_full[st % kStages], (st / kStages) & 1, sh, status);
+                if (!__all_sync(0xffffffffu, ok)) {
+                    ok = false;
+                    break;
+                }
+                tc_after();
+                if (elect_one()) {
+                    const uint64_t kd = k_desc + (st & 1) * kStage;
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k)
-                        tc_mma(tmem + (st & 1) * kKeys, tile_desc(q_s + (k / 4) * (kRows * 128) + (k % 4) * 32, 16),
-                               tile_desc(k_at + (k / 4) * (kKeys * 128) + (k % 4) * 32, 16), kS, k > 0);
+                        tc_mma(tm + (st & 1) * kKeys, q_desc + ((k / 4) * (kRows * 128) + (k % 4) * 32 >> 4), kd + ((k / 4) * (kKeys * 128) + (k % 4) * 32 >> 4), kS, k > 0);
                     tc_commit(&sh->s_full[st & 1]);
-                    tc_commit(&sh->k_empty[st % kStages]);
+                    tc_commit(&sh->k_empty[st & 1]);
                 }
-                if (st > 0) {
-                    const int pv = st - 1;
-                    ok = wait_bar(&sh->p_full[pv & 1], (pv >> 1) & 1, sh, status) && wait_bar(&sh->v_full[pv % kStages], (pv / kStages) & 1, sh, status);
-                    if (!ok) break;
-                    tc_after();
-                    const uint32_t v_at = kv_s + (pv % kStages) * 2 * S::kKV + S::kKV;
+                __syncwarp();
+            }
+            if (st > 0) {
+                const int pv = st - 1;
+                ok = wait_bar(&sh->p_full[pv & 1], (pv >> 1) & 1, sh, status) && wait_bar(&sh->v_full[pv % kStages], (pv / kStages) & 1, sh, status);
+                if (!__all_sync(0xffffffffu, ok)) {
+                    ok = false;
+                    break;
+                }
+                tc_after();
+                if (elect_one()) {
+                    const uint64_t vd = v_desc + (pv & 1) * kStage;
 #pragma unroll
-                    for (int k = 0; k < kKeys / 16; ++k)
-                        tc_mma_ta(tmem + 2 * kKeys, tmem + (pv & 1) * kKeys + k * 8, tile_desc(v_at + k * 2048, kKeys * 128), kO, pv > 0 || k > 0);
-                    tc_commit(&sh->v_empty[pv % kStages]);
+                    for (int k = 0; k < kKeys / 16; ++k) tc_mma_ta(tm + 2 * kKeys, tm + (pv & 1) * kKeys + k * 8, vd + k * (2048 >> 4), kO, pv > 0 || k > 0);
+                    tc_commit(&sh->v_empty[pv & 1]);
                     tc_commit(&sh->p_empty);
                 }
+                __syncwarp();
             }
-            // nothing may be under way when tensor memory is freed
-            tc_commit(&sh->drain);
-            for (unsigned i = 0; i < kSpins; ++i)
-                if (mbar_try(smem_u32(&sh->drain), 0)) break;
         }
+        // nothing may be under way when tensor memory is freed
+        if (elect_one()) tc_commit(&sh->drain);
+        __syncwarp();
+        for (unsigned i = 0; i < kSpins; ++i)
+            if (mbar_try(smem_u32(&sh->drain), 0)) break;
     } else {
         // ---- softmax: one row per thread ----
         const int row = warp * 32 + lane, j = min(row / a.group, n), lim = row < nrows ? max(pos0 + j + 1, 0) : 0;
