@@ -108,6 +108,7 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
     __shared__ struct { long long first, end, total, ctas, at, tile_base; int units, head, u0, u1, t; } s_line_;
     volatile auto& s_line = s_line_;
     __shared__ int s_last;
+    __shared__ int s_again[R];                // rows that are not finite, where that may come from keys of other rows
     __shared__ volatile int s_dead[kWarps];   // a bounded wait of the warp ran out
 
     const Cache& c = a.c;
@@ -649,6 +650,10 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
         }
         if (!kInt4) cp_async_wait<0>();
 
+        // A tile of several tokens multiplies the last tokens' values with zeros of the earlier ones: a value that is not finite spoils them, and
+        // rows that come out so are done again over their own keys alone.
+        const bool shared_end = !kInt4 && !LIST && lim_lo < lim_hi;
+        if (shared_end && tid < R) s_again[tid] = 0;
         // ---- the warps' results side by side: [row][d], rows padded by 4 words ----
         __syncwarp();
         float* so = reinterpret_cast<float*>(ring);
@@ -684,7 +689,10 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
             const bool nan = lsum != lsum;
             float y[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = nan ? lsum : x[i] * inv;
+            for (int i = 0; i < 4; ++i) {
+                y[i] = nan ? lsum : x[i] * inv;
+                if (shared_end && !(fabsf(y[i]) < INFINITY)) s_again[row] = 1;
+            }
             w.x = (uint32_t)to_bits(y[0], bf) | (uint32_t)to_bits(y[1], bf) << 16;
             w.y = (uint32_t)to_bits(y[2], bf) | (uint32_t)to_bits(y[3], bf) << 16;
             *reinterpret_cast<uint2*>(a.out + 2 * (orow * D + d0)) = w;
@@ -770,6 +778,15 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
                     }
                     write_out(row, d0, x, ls, mx);
                 }
+            }
+        }
+        if (shared_end) {
+            __syncthreads();
+            for (int row = warp; row < rows; row += kWarps) {
+                if (!s_again[row]) continue;
+                const int rr = tl.row0 + row, lim = tl.limit(rr, a.group);
+                plain_row<BF, D>(a, tl.tok0 + rr / a.group, head * a.group + rr % a.group, lim, (lim + c.page - 1) >> c.page_shift, lane,
+                                 [&](int e) { return make_int2(e, page_of(a.b, c, tl.r, e, status)); });
             }
         }
         const long long next = s_line.at + (s_line.u1 - part0);

@@ -11,8 +11,9 @@
 // the previous step's values', so that it runs while the softmax does.  Two CTAs share an SM (d <= 128).  The running maximum moves only
 // when a logit exceeds it by more than 2^8, so that O is hardly ever read back to be scaled.
 //
-// A zero p must not meet an infinity or a not-a-number among the values of a block that the row did not list: the loading warps look
-// at every value, and a tile that holds such a one is done again row by row with plain arithmetic, each row over its own keys only.
+// A zero p must not meet an infinity or a not-a-number among the values of a block that the row did not list.  Such a value leaves its mark in
+// O of every row, since no product of it is finite; rows of O that are not finite are done again with plain arithmetic over their own keys
+// only.  (Looking at every value as it came cost 18 of 211 us.)
 //
 // Every wait is bounded: one that runs out raises the status flag, all roles leave, and tensor memory is freed.
 #include <type_traits>
@@ -49,7 +50,8 @@ struct TileShared {
     unsigned long long k_full[kStages], v_full[kStages], k_empty[kStages], v_empty[kStages], s_full[2];
     uint32_t tmem;
     volatile int abort;      // a wait ran out
-    volatile int special;    // a value is not finite
+    volatile int special;    // a row of O is not finite
+    unsigned char again[kRows];
     int count[kThreads / 32];
 };
 
@@ -216,7 +218,6 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
         auto run = [&](auto which) {
             constexpr bool V = decltype(which)::value;
             constexpr int N = 32 * (V ? kValueWarps : kKeyWarps), RS = N / CH > 0 ? N / CH : 1;      // threads; rows per pass
-            constexpr uint32_t EXP = BF ? 0x7f807f80u : 0x7c007c00u, ONE = BF ? 0x00800080u : 0x04000400u;
             const int t = tid - 32 * (kSoftWarps + 1 + (V ? kKeyWarps : 0)), ch = t % CH, row0 = t / CH;
             if (V) {
                 for (int row = row0; row < kRows; row += RS) {
@@ -232,7 +233,6 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
             }
             const int64_t s0 = V ? c.vs[0] : c.ks[0], s1 = V ? c.vs[1] : c.ks[1], s2 = V ? c.vs[2] : c.ks[2];
             const char* src0 = (V ? c.v : c.k) + 2 * (head * s1 + ch * 8);
-            uint32_t special = 0;
             for (int st = 0; st < nstep; ++st) {
                 const int slot = st % kStages;
                 if (st >= kStages && !wait_bar<true>(V ? &sh->v_empty[slot] : &sh->k_empty[slot], ((st / kStages) & 1) ^ 1, sh, status)) break;
@@ -259,18 +259,8 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
                 cp_async_wait<0>();
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 mbar_arrive(smem_u32(V ? &sh->v_full[slot] : &sh->k_full[slot]));
-                if (V) {
-                    // the product only reads the tile, so it may be looked at meanwhile; the slot is written again by these threads
-#pragma unroll 8
-                    for (int row = row0; row < kKeys; row += RS) {
-                        uint32_t x, y, z, w;
-                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x), "=r"(y), "=r"(z), "=r"(w) : "r"(dst + row * 128 + (((ch & 7) ^ (row & 7)) * 16)) : "memory");
-                        special |= (((x & EXP) + ONE) | ((y & EXP) + ONE) | ((z & EXP) + ONE) | ((w & EXP) + ONE)) & 0x80008000u;
-                    }
-                }
             }
             cp_async_wait<0>();
-            if (special) sh->special = 1;
         };
         if (values) run(std::true_type{});
         else run(std::false_type{});
@@ -332,24 +322,28 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
         const int row = warp * 32 + lane, j = min(row / a.group, n), lim = row < nrows ? max(pos0 + j + 1, 0) : 0;
         const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
         const float fscale = fmaxf(a.scale, 1e-30f) * kLog2e;      // a masked product is -infinity and has to stay it
+        // keys of a step that the row sees, as bits; found for the next step while this one's P is on its way
+        auto seen_of = [&](int st) -> unsigned long long {
+            if (row >= nrows || st >= nstep) return 0ull;
+            if (pieces == 1) {
+                const int e = st >> half_shift;
+                if (!(s_mask[e] >> j & 1ull)) return 0ull;
+                const int v = lim - ((s_list[e].x << c.page_shift) + (st & (halves - 1)) * kKeys);
+                return v >= kKeys ? ~0ull : v <= 0 ? 0ull : (1ull << v) - 1ull;
+            }
+            unsigned long long bits = 0ull;
+            for (int i = 0; i < pieces; ++i) {
+                const int e = st * pieces + i;
+                if (e >= total || !(s_mask[e] >> j & 1ull)) continue;
+                const int v = min(max(lim - (s_list[e].x << c.page_shift), 0), piece);
+                bits |= ((1ull << v) - 1ull) << (i * piece);
+            }
+            return bits;
+        };
         float m = -INFINITY, l = 0.f;
         bool ok = true;
+        unsigned long long seen = seen_of(0);
         for (int st = 0; st < nstep && ok; ++st) {
-            // keys of the row in the step: `seen` bits
-            unsigned long long seen = 0ull;
-            if (row < nrows) {
-                if (pieces == 1) {
-                    const int e = st >> half_shift, v = min(max(lim - ((s_list[e].x << c.page_shift) + (st & (halves - 1)) * kKeys), 0), kKeys);
-                    if (s_mask[e] >> j & 1ull) seen = v == kKeys ? ~0ull : (1ull << v) - 1ull;
-                } else {
-                    for (int i = 0; i < pieces; ++i) {
-                        const int e = st * pieces + i;
-                        if (e >= total || !(s_mask[e] >> j & 1ull)) continue;
-                        const int v = min(max(lim - (s_list[e].x << c.page_shift), 0), piece);
-                        seen |= ((1ull << v) - 1ull) << (i * piece);
-                    }
-                }
-            }
             ok = wait_bar(&sh->s_full[st & 1], (st >> 1) & 1, sh, status);
             if (!__all_sync(0xffffffffu, ok)) {
                 ok = false;
@@ -419,6 +413,7 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
             tc_store32(lanes + (st & 1) * kKeys, packed);
             tc_before();
             mbar_arrive(smem_u32(&sh->p_full[st & 1]));
+            seen = seen_of(st + 1);
         }
         if (ok && nstep > 0) ok = wait_bar(&sh->drain, 0, sh, status);      // all products are done
         ok = __all_sync(0xffffffffu, ok);
@@ -427,10 +422,15 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
         const bool nan = l != l;
         const float inv = nan ? l : l > 0.f ? 1.f / l : 0.f;
         const int64_t orow = (int64_t)(tok0 + row / a.group) * (c.nheads * a.group) + head * a.group + row % a.group;
+        bool finite = true;
         for (int cc = 0; cc < D; cc += 32) {
             uint32_t x[32];
             if (nstep > 0) tc_load32(lanes + 2 * kKeys + cc, x);
             if (row < nrows) {
+                if (nstep > 0) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) finite = finite && fabsf(__uint_as_float(x[i])) < INFINITY;
+                }
 #pragma unroll
                 for (int i = 0; i < 32; i += 8) {
                     float y[8];
@@ -440,6 +440,8 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
                 }
             }
         }
+        sh->again[row] = row < nrows && !finite;
+        if (row < nrows && !finite) sh->special = 1;
         if (a.lse && row < nrows) a.lse[orow] = nan ? l : l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
         tc_before();
     }
@@ -449,38 +451,12 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kCols) : "memory");
     }
     if (sh->special && !sh->abort) {
-        // ---- a value is not finite: every row over its own keys, a warp per row ----
-        constexpr int E = D / 32;
+        // ---- rows that are not finite: over their own keys, a warp per row ----
         for (int row = warp; row < nrows; row += kThreads / 32) {
-            const int j = row / a.group, h = head * a.group + row % a.group, lim = pos0 + j + 1, e0 = lane * E;
-            float q[E], o[E], m = -INFINITY, l = 0.f;
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                q[i] = to_float(reinterpret_cast<const uint16_t*>(a.q.p + 2 * ((int64_t)(tok0 + j) * a.q.ts + (int64_t)h * a.q.hs))[e0 + i], BF) * a.scale * kLog2e;
-                o[i] = 0.f;
-            }
-            for (int e = 0; e < total; ++e) {
-                if (!(s_mask[e] >> j & 1ull)) continue;
-                const int2 en = s_list[e];
-                const int end = min(c.page, lim - (en.x << c.page_shift));
-                for (int t = 0; t < end; ++t) {
-                    const uint16_t* kp = reinterpret_cast<const uint16_t*>(c.k) + en.y * c.ks[0] + head * c.ks[1] + t * c.ks[2] + e0;
-                    const uint16_t* vp = reinterpret_cast<const uint16_t*>(c.v) + en.y * c.vs[0] + head * c.vs[1] + t * c.vs[2] + e0;
-                    float x = 0.f;
-#pragma unroll
-                    for (int i = 0; i < E; ++i) x = fmaf(q[i], to_float(kp[i], BF), x);
-#pragma unroll
-                    for (int s = 16; s; s >>= 1) x += __shfl_xor_sync(0xffffffffu, x, s);
-                    const float mn = fmaxf(m, x), f = m == mn ? 1.f : ex2(m - mn), pr = ex2(x - mn);
-                    m = mn;
-                    l = fmaf(l, f, pr);
-#pragma unroll
-                    for (int i = 0; i < E; ++i) o[i] = fmaf(pr, to_float(vp[i], BF), o[i] * f);
-                }
-            }
-            const int64_t orow = (int64_t)(tok0 + j) * (c.nheads * a.group) + h;
-#pragma unroll
-            for (int i = 0; i < E; ++i) reinterpret_cast<uint16_t*>(a.out)[orow * D + e0 + i] = to_bits(l == 0.f ? 0.f : o[i] / l, BF);
+            if (!sh->again[row]) continue;
+            const int j = row / a.group;
+            plain_row<BF, D>(a, tok0 + j, head * a.group + row % a.group, pos0 + j + 1, total, lane,
+                             [&](int e) { return s_mask[e] >> j & 1ull ? s_list[e] : make_int2(0, -1); });
         }
     }
 }

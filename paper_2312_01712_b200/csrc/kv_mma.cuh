@@ -91,5 +91,42 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
+// One row of a 16-bit cache with plain arithmetic, by a warp: the keys before `lim` of the blocks that entry(i) -> (block, page) names,
+// i < count, page < 0: none.  For rows that a product over several rows' keys has spoilt: 0 times a value that is not finite.
+template <bool BF, int D, class Entry>
+__device__ __forceinline__ void plain_row(const AttendArgs& a, int tok, int h, int lim, int count, int lane, Entry entry) {
+    constexpr int E = D / 32;
+    const Cache& c = a.c;
+    const int head = h / a.group, e0 = lane * E;
+    float q[E], o[E], m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        q[i] = to_float(reinterpret_cast<const uint16_t*>(a.q.p + 2 * ((int64_t)tok * a.q.ts + (int64_t)h * a.q.hs))[e0 + i], BF) * a.scale * kLog2e;
+        o[i] = 0.f;
+    }
+    for (int e = 0; e < count; ++e) {
+        const int2 en = entry(e);
+        if (en.y < 0) continue;
+        const int end = min(c.page, lim - (en.x << c.page_shift));
+        for (int t = 0; t < end; ++t) {
+            const uint16_t* kp = reinterpret_cast<const uint16_t*>(c.k) + en.y * c.ks[0] + head * c.ks[1] + t * c.ks[2] + e0;
+            const uint16_t* vp = reinterpret_cast<const uint16_t*>(c.v) + en.y * c.vs[0] + head * c.vs[1] + t * c.vs[2] + e0;
+            float x = 0.f;
+#pragma unroll
+            for (int i = 0; i < E; ++i) x = fmaf(q[i], to_float(kp[i], BF), x);
+#pragma unroll
+            for (int s = 16; s; s >>= 1) x += __shfl_xor_sync(0xffffffffu, x, s);
+            const float mn = fmaxf(m, x), f = m == mn ? 1.f : ex2(m - mn), pr = ex2(x - mn);
+            m = mn;
+            l = fmaf(l, f, pr);
+#pragma unroll
+            for (int i = 0; i < E; ++i) o[i] = fmaf(pr, to_float(vp[i], BF), o[i] * f);
+        }
+    }
+    const int64_t row = (int64_t)tok * (c.nheads * a.group) + h;
+#pragma unroll
+    for (int i = 0; i < E; ++i) reinterpret_cast<uint16_t*>(a.out)[row * D + e0 + i] = to_bits(l == 0.f ? 0.f : o[i] / l, BF);
+}
+
 }  // namespace kv
 }  // namespace ivfpq

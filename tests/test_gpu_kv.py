@@ -161,6 +161,52 @@ def test_attend_long_prompt_over_listed_blocks(fmt, dtype):
     s.check(torch.from_numpy(blocks).cuda())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("page,G", [(16, 4), (64, 8), (128, 3), (32, 1)])
+def test_values_that_are_not_finite_stay_with_the_rows_that_see_them(dtype, page, G):
+    # held infinities and not-a-numbers in a block, and in tokens of the prompt's own end: a token that did not list the
+    # block, or comes before the token, must not notice
+    n = 6 * page + 40
+    s = Setup(dtype, dtype, page=page, G=G, lens=(n, 3 * page), news=(100, 2 * page), seed=page)
+    bad_block, bad_pos = 2, n - 30
+    for name in ("k", "v"):
+        x = s.tensors[name]
+        x[int(s.table[0, bad_block]), :, 5] = float("nan") if name == "k" else float("inf")
+        x[int(s.table[0, bad_pos // page]), :, bad_pos % page] = float("nan")
+    rng = np.random.default_rng(3)
+    blocks = np.full((s.ntok, s.hkv, 4), -1, np.int32)
+    touched = np.zeros((s.ntok, s.hkv), bool)
+    for t, (r, pos) in enumerate(s.pos):
+        for h in range(s.hkv):
+            pick = np.unique(np.concatenate((rng.permutation(pos // page + 1)[:3], [pos // page])))
+            blocks[t, h, :len(pick)] = pick
+            touched[t, h] = r == 0 and ((bad_block in pick and pos >= bad_block * page + 5) or (pos >= bad_pos and bad_pos // page in pick))
+    bt = torch.from_numpy(blocks).cuda()
+    out = lib.ivfpq_kv_attend(s.cache, s.batch, s.q, blocks=bt)
+    clean, _, mag, big = ref.attend(s.kref, s.vref, s.table, s.lens, s.q_start, s.q, page, None, bt)
+    free = torch.from_numpy(~touched).cuda().repeat_interleave(G, 1)
+    assert bool(free.any()) and bool((~free).any())
+    tol = ROUND[s.dt] * clean.abs() + mag * (2 * ROUND[s.dt] * 1.05 + 2 * (big * 144 * 2.0 ** -24 + 2.0 ** -20)[..., None]) + 1e-4
+    assert bool(((out.double() - clean).abs() <= tol)[free].all())
+    assert bool(torch.isnan(out)[~free].any(-1).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("G", [1, 3, 8, 16])
+def test_tokens_do_not_notice_later_ones_that_are_not_finite(dtype, G):
+    # drafted tokens over the whole cache: the last token's key and value are not finite
+    s = Setup(dtype, dtype, G=G, lens=(150, 37, 64), news=(5, 4, 6), seed=G)
+    for r, n in enumerate(s.lens):
+        for name in ("k", "v"):
+            s.tensors[name][int(s.table[r, (n - 1) // s.page]), :, (n - 1) % s.page] = float("nan") if r else float("inf")
+    out = lib.ivfpq_kv_attend(s.cache, s.batch, s.q)
+    clean, _, mag, big = ref.attend(s.kref, s.vref, s.table, s.lens, s.q_start, s.q, s.page)
+    last = torch.tensor([pos == s.lens[r] - 1 for r, pos in s.pos], device="cuda")
+    tol = ROUND[s.dt] * clean.abs() + mag * (2 * ROUND[s.dt] * 1.05 + 2 * (big * 144 * 2.0 ** -24 + 2.0 ** -20)[..., None]) + 1e-4
+    assert bool(((out.double() - clean).abs() <= tol)[~last].all())
+    assert bool(torch.isnan(out)[last].any(-1).all())
+
+
 def test_attend_scales_and_wide_logits():
     for fmt, dtype in (("int4", "fp16"), ("bf16", "bf16")):
         s = Setup(fmt, dtype, lens=(300, 40), seed=3)
