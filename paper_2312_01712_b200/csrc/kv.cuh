@@ -142,6 +142,9 @@ __device__ __forceinline__ int8_t code8(float x, float factor) {
     return y == y ? (int8_t)__float2int_rn(fminf(fmaxf(y, -127.f), 127.f)) : (int8_t)0;
 }
 
+// Streaming multiprocessors of the current device.
+cudaError_t sm_count(int* sms);            // kv_api.cu
+
 // Launchers.
 cudaError_t launch_append(const Cache& c, const Batch& b, bool bf16, const Rows& k, const Rows& v, int* status, cudaStream_t st);
 cudaError_t launch_read(const Cache& c, const Batch& b, bool bf16, char* k, char* v, int* status, cudaStream_t st);

@@ -85,6 +85,26 @@ int done(cudaError_t e) { return e == cudaSuccess ? IVFPQ_OK : IVFPQ_ERR_CUDA; }
 
 }  // namespace
 
+namespace ivfpq {
+namespace kv {
+
+cudaError_t sm_count(int* sms) {
+    static int known[64];                          // by device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 64 && known[dev]) {
+        *sms = known[dev];
+        return cudaSuccess;
+    }
+    e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess && dev < 64) known[dev] = *sms;
+    return e;
+}
+
+}  // namespace kv
+}  // namespace ivfpq
+
 extern "C" {
 
 size_t ivfpq_kv_workspace_bytes(int32_t d) {

@@ -137,6 +137,11 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
     };
 
     // ---- the CTA's part of the line of units ----
+    // Little work in all: parts are whole runs of kRun units, so that short requests are not cut (a cut costs a ticket and a join, more
+    // than the few units it spreads).
+    constexpr int kRun = 4;
+    int run = 1;
+    auto runs_of = [&](int t, Tile* tl) -> int { return (units_of(t, tl) + run - 1) / run; };
     long long total = 0, first = 0, end = 0, tile_base = 0;   // tile_base: first unit of tile `t`
     long long ctas = 1;                                       // that have a part: none is empty
     int t = 0;
@@ -150,48 +155,76 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
     };
     if (plan.whole) {
         t = blockIdx.x;
-        const int units = units_of(t, &tl);
+        const int units = runs_of(t, &tl);
         if (units == 0) return;
         first = (long long)blockIdx.y * units;
         end = first + units;
     } else {
-        // every thread sums a run of tiles; the one whose run holds the CTA's first unit finds the tile
-        const int per = (plan.ntiles + kThreads - 1) / kThreads;
-        const int t_lo = min(tid * per, plan.ntiles), t_hi = min(t_lo + per, plan.ntiles);
-        long long sum = 0;
-        for (int i = t_lo; i < t_hi; ++i) {
+        if (plan.ntiles <= 32) {
+            // a tile per lane: every warp finds the CTA's part by itself, without a barrier
             Tile x;
-            sum += units_of(i, &x);
-        }
-        sum *= c.nheads;
-        long long inc = sum;
-        if (plan.ntiles > 1) {
+            const int n = lane < plan.ntiles ? units_of(lane, &x) : 0;
+            const long long few = (long long)kRun * gridDim.x;
+            long long sum = __reduce_add_sync(0xffffffffu, min(n, 1 << 24));
+            if (sum * c.nheads <= few) run = kRun;
+            long long inc = (long long)((n + run - 1) / run) * c.nheads;
+            const long long mine = inc;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const long long y = __shfl_up_sync(0xffffffffu, inc, o);
                 if (lane >= o) inc += y;
             }
-        }
-        if (plan.ntiles > 1 ? lane == 31 : tid == 0) s_scan[warp] = inc;
-        __syncthreads();
-        long long base = inc - sum;
-        if (plan.ntiles > 1) {
+            total = __shfl_sync(0xffffffffu, inc, 31);
+            ctas = min((long long)gridDim.x, total);
+            if (blockIdx.x >= ctas) return;
+            first = share(blockIdx.x, total, ctas);
+            end = share(blockIdx.x + 1, total, ctas);
+            t = __ffs(__ballot_sync(0xffffffffu, first < inc)) - 1;
+            tile_base = __shfl_sync(0xffffffffu, inc - mine, t);
+        } else {
+            // every thread sums a run of tiles; the one whose run holds the CTA's first unit finds the tile
+            const int per = (plan.ntiles + kThreads - 1) / kThreads;
+            const int t_lo = min(tid * per, plan.ntiles), t_hi = min(t_lo + per, plan.ntiles);
+            long long sum = 0, sum_runs = 0;
+            for (int i = t_lo; i < t_hi; ++i) {
+                Tile x;
+                const int n = units_of(i, &x);
+                sum += n;
+                sum_runs += (n + kRun - 1) / kRun;
+            }
+            const long long few = (long long)kRun * gridDim.x;
+            if (!__syncthreads_or(sum > few)) {                      // the sum fits 32 bits: is it few in all?
+                const int in_warp = __reduce_add_sync(0xffffffffu, (int)sum);
+                if (lane == 0) s_scan[warp] = in_warp;
+                __syncthreads();
+                long long all = 0;
+                for (int w = 0; w < kWarps; ++w) all += s_scan[w];
+                if (all * c.nheads <= few) run = kRun;
+                __syncthreads();
+            }
+            if (run > 1) sum = sum_runs;
+            sum *= c.nheads;
+            long long inc = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, inc, o);
+                if (lane >= o) inc += y;
+            }
+            if (lane == 31) s_scan[warp] = inc;
+            __syncthreads();
+            long long base = inc - sum;
             for (int w = 0; w < kWarps; ++w) {
                 if (w < warp) base += s_scan[w];
                 total += s_scan[w];
             }
-        } else {
-            total = s_scan[0];
-        }
-        ctas = min((long long)gridDim.x, total);
-        if (blockIdx.x >= ctas) return;
-        first = share(blockIdx.x, total, ctas);
-        end = share(blockIdx.x + 1, total, ctas);
-        if (plan.ntiles > 1) {
+            ctas = min((long long)gridDim.x, total);
+            if (blockIdx.x >= ctas) return;
+            first = share(blockIdx.x, total, ctas);
+            end = share(blockIdx.x + 1, total, ctas);
             if (base <= first && first < base + sum) {
                 for (int i = t_lo; i < t_hi; ++i) {
                     Tile x;
-                    const long long n = (long long)units_of(i, &x) * c.nheads;
+                    const long long n = (long long)runs_of(i, &x) * c.nheads;
                     if (first < base + n) {
                         s_line.t = i;
                         s_scan[kWarps] = base;
@@ -205,7 +238,6 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
             tile_base = s_scan[kWarps];
         }
     }
-
     if (tid == 0) {
         s_line.first = first;
         s_line.end = end;
@@ -215,25 +247,21 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
         s_line.tile_base = tile_base;
         s_line.t = t;
     }
-    __syncthreads();
 
-    for (;;) {
+    for (long long at = first;;) {
         int head, u0, u1;
         {
-            const long long at = s_line.at, end = s_line.end;
-            long long tile_base = s_line.tile_base;
-            int t = s_line.t, units = units_of(t, &tl);
+            int units = runs_of(t, &tl);
             const int t0 = t;
             while (at >= tile_base + (long long)units * c.nheads) {      // next tile with work
                 tile_base += (long long)units * c.nheads;
                 ++t;
-                units = units_of(t, &tl);
+                units = runs_of(t, &tl);
             }
             head = (int)((unsigned)(at - tile_base) / (unsigned)units);  // units * heads < 2^31: checked at the launch
             u0 = (int)(at - tile_base - (long long)head * units);
             u1 = (int)min((long long)units, u0 + (end - at));
-            __syncthreads();
-            if (tid == 0) {
+            if (tid == 0) {                        // read behind the segment's barriers
                 if (t != t0) {
                     s_line.t = t;
                     s_line.tile_base = tile_base;
@@ -250,14 +278,14 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
         const int32_t* list = LIST ? a.blocks + ((int64_t)tl.tok0 * c.nheads + head) * a.nselect : nullptr;
 
         // ---- 16-key pieces of the warp: piece s covers (virtual) keys (u0 + s / 2) 128 + 32 warp + 16 (s % 2) ----
-        const int nsub = (u1 - u0) * 2, nstage = nsub / S::kSubs;
+        const int nsub = (u1 - u0) * run * 2, nstage = nsub / S::kSubs;      // those past the last key are passed over
         const char *k_cur = nullptr, *k_nxt = nullptr, *v_cur = nullptr, *v_nxt = nullptr;   // where piece (batch, lane) is held
         int pos_cur = 0, pos_nxt = 0;         // and the position of its first key
         auto look = [&](int s, const char** kp, const char** vp, int* pos) {
             *kp = nullptr;
             *pos = lim_hi;                    // no key: masked throughout
             if (s >= nsub || (kInt4 && s_dead[warp])) return;
-            const int vk = (u0 + (s >> 1)) * kUnit + warp * 32 + (s & 1) * 16;
+            const int vk = (u0 * run + (s >> 1)) * kUnit + warp * 32 + (s & 1) * 16;
             if (vk >= vlen) return;
             int blk = vk >> c.page_shift;
             if (LIST) {
@@ -791,8 +819,12 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
         }
         const long long next = s_line.at + (s_line.u1 - part0);
         if (next >= s_line.end) break;
-        __syncthreads();                      // the rings hold O until here
+        __syncthreads();                      // the rings hold O until here, and everybody has read the line
         if (tid == 0) s_line.at = next;
+        at = next;
+        end = s_line.end;
+        t = s_line.t;
+        tile_base = s_line.tile_base;
         __syncthreads();
     }
     // Every copy was waited for above, unless a wait ran out: then wait once more for all slots, again within a limit.
@@ -868,9 +900,8 @@ size_t attend_workspace_bytes(int d) { return (size_t)2 * kMaxCtas * 16 * (d + 2
 cudaError_t launch_attend(const AttendArgs& a, cudaStream_t st) {
     static_assert(256 + kMaxCtas * 4 <= kZeroBytes, "tickets");
     if (attend_tile_serves(a)) return launch_attend_tile(a, st);
-    int dev = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    int sms = 0;
+    const cudaError_t e = sm_count(&sms);
     if (e != cudaSuccess) return e;
     if (a.c.format == IVFPQ_KV_INT4) return pick_width<IVFPQ_KV_INT4>(a, sms, st);
     if (a.c.format == IVFPQ_KV_BF16) return pick_width<IVFPQ_KV_BF16>(a, sms, st);

@@ -476,9 +476,8 @@ cudaError_t pick_columns(const SelectArgs& a, int sms, cudaStream_t st) {
 }  // namespace
 
 cudaError_t launch_select(const SelectArgs& a, cudaStream_t st) {
-    int dev = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    int sms = 0;
+    const cudaError_t e = sm_count(&sms);
     if (e != cudaSuccess) return e;
     if (a.c.d == 64) return pick_columns<64>(a, sms, st);
     if (a.c.d == 128) return pick_columns<128>(a, sms, st);

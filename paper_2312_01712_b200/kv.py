@@ -37,6 +37,10 @@ class ivfpq_kv_batch_t(ctypes.Structure):
                 ("block_table", ctypes.c_void_p), ("seq_len", ctypes.c_void_p), ("q_start", ctypes.c_void_p)]
 
 
+# torch.cuda.current_stream() builds a Stream object, 2 us of a call that takes 10
+_current_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -99,13 +103,15 @@ class KvCacheHandle:
                 raise ValueError("bounds must be int8 [pages, heads, 2, d] and bounds_scale fp32 [pages, heads], contiguous, on the cache's device")
             s.bounds, s.bounds_scale = bounds.data_ptr(), bounds_scale.data_ptr()
         self.struct, self.format, self.d, self.page, self.npages, self.nheads = s, s.format, s.d, s.page, s.npages, s.nheads
-        self.device, self.dtype = first.device, _HELD.get(s.format)
+        self.device, self.dtype, self._any = first.device, _HELD.get(s.format), first
         self.records, self.k, self.v, self.bounds, self.bounds_scale = records, k, v, bounds, bounds_scale
         self._ref = ctypes.addressof(s)
         self._nbytes = ivfpq_kv_workspace_bytes(s.d)
         if self._nbytes == 0 or s.page not in (16, 32, 64, 128):
             raise IvfpqError(IVFPQ_ERR_UNSUPPORTED, "KvCacheHandle")
         self._ws: dict = {}
+        self._at: dict = {}          # addresses of the workspaces
+        self._index = first.device.index
 
     @classmethod
     def empty(cls, npages: int, nheads: int, page: int, d: int, dtype=None, bounds: bool = True, device="cuda") -> "KvCacheHandle":
@@ -127,9 +133,11 @@ class KvCacheHandle:
         return ws
 
     def _call(self) -> Tuple[int, int]:
-        stream = torch.cuda.current_stream(self.device).cuda_stream
-        ws = self._ws.get(stream)
-        return stream, (self.workspace(stream) if ws is None else ws).data_ptr()
+        stream = _current_stream(self._index)
+        at = self._at.get(stream)
+        if at is None:
+            at = self._at[stream] = self.workspace(stream).data_ptr()
+        return stream, at
 
 
 class KvBatchHandle:
@@ -170,7 +178,7 @@ def ivfpq_kv_read(cache: KvCacheHandle, batch: KvBatchHandle, ntok: int, dtype: 
     """The held keys and values of the step's `ntok` tokens, each [tokens, heads, d]."""
     if out is None:
         dtype = dtype or cache.dtype or torch.bfloat16
-        out = tuple(torch.empty((ntok, cache.nheads, cache.d), dtype=dtype, device=cache.device) for _ in range(2))
+        out = tuple(cache._any.new_empty((ntok, cache.nheads, cache.d), dtype=dtype) for _ in range(2))
     k, v = out
     if k.shape[0] != ntok:
         raise ValueError("out must have ntok rows")
@@ -187,8 +195,9 @@ def ivfpq_kv_read_bounds(cache: KvCacheHandle, pages: torch.Tensor):
     """Upper and lower bounds of the keys of physical `pages` (int32 [n]), each fp32 [n, heads, d]."""
     if pages.dtype != torch.int32 or pages.dim() != 1 or not pages.is_contiguous() or pages.device != cache.device:
         raise ValueError("pages must be a contiguous int32 tensor on the cache's device")
-    hi = torch.empty((pages.shape[0], cache.nheads, cache.d), dtype=torch.float32, device=cache.device)
-    lo = torch.empty_like(hi)
+    if cache.bounds is None:
+        raise ValueError("the cache keeps no bounds")
+    hi, lo = (cache.bounds_scale.new_empty((pages.shape[0], cache.nheads, cache.d)) for _ in range(2))
     stream, ws = cache._call()
     _check(_load().ivfpq_kv_read_bounds(cache._ref, pages.data_ptr(), pages.shape[0], hi.data_ptr(), lo.data_ptr(), ws, cache._nbytes,
                                         stream), "ivfpq_kv_read_bounds")
@@ -201,7 +210,7 @@ def ivfpq_kv_select(cache: KvCacheHandle, batch: KvBatchHandle, q: torch.Tensor,
     [tokens, query heads, d]."""
     dt = _rows(q, cache, "q")
     if out is None:
-        out = torch.empty((q.shape[0], cache.nheads, nselect), dtype=torch.int32, device=q.device)
+        out = q.new_empty((q.shape[0], cache.nheads, nselect), dtype=torch.int32)
     elif out.dtype != torch.int32 or tuple(out.shape) != (q.shape[0], cache.nheads, nselect) or not out.is_contiguous() \
             or out.device != cache.device:
         raise ValueError("out must be a contiguous int32 tensor [tokens, kv heads, nselect] on the cache's device")
@@ -219,7 +228,7 @@ def ivfpq_kv_attend(cache: KvCacheHandle, batch: KvBatchHandle, q: torch.Tensor,
     is filled if given."""
     dt = _rows(q, cache, "q")
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(q.shape)
     elif out.dtype != q.dtype or out.shape != q.shape or not out.is_contiguous() or out.device != cache.device:
         raise ValueError("out must be a contiguous tensor like q")
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.device != cache.device):
@@ -241,7 +250,7 @@ def ivfpq_kv_attend(cache: KvCacheHandle, batch: KvBatchHandle, q: torch.Tensor,
 
 def ivfpq_kv_status(cache: KvCacheHandle) -> int:
     """Synchronises the current stream and returns (and clears) the device status of the calls made on it."""
-    stream = torch.cuda.current_stream(cache.device).cuda_stream
+    stream = _current_stream(cache._index)
     if stream not in cache._ws:
         return binding.IVFPQ_OK
     return int(_load().ivfpq_kv_status(cache._ws[stream].data_ptr(), stream))
