@@ -128,6 +128,32 @@ __device__ __forceinline__ uint4 pack8(const float* x, bool bf16) {
     for (int i = 0; i < 4; ++i) u[i] = (uint32_t)to_bits(x[2 * i], bf16) | (uint32_t)to_bits(x[2 * i + 1], bf16) << 16;
     return make_uint4(u[0], u[1], u[2], u[3]);
 }
+// The same for a type known when compiling: one instruction per element, and per pair.
+template <bool BF>
+__device__ __forceinline__ void unpack8(const uint4& w, float* x) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (BF) {
+            x[2 * i] = __uint_as_float(u[i] << 16);
+            x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+        } else {
+            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+            x[2 * i] = y.x;
+            x[2 * i + 1] = y.y;
+        }
+    }
+}
+template <bool BF>
+__device__ __forceinline__ uint4 pack8(const float* x) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (BF) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u[i]) : "f"(x[2 * i + 1]), "f"(x[2 * i]));
+        else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(u[i]) : "f"(x[2 * i + 1]), "f"(x[2 * i]));
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
 // What 8 codes of a word stand for (s * u exact in fp32: one rounding).
 __device__ __forceinline__ void decode8(uint32_t w, float s, float z, float* x) {
 #pragma unroll

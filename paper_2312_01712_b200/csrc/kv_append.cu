@@ -1,4 +1,6 @@
 // Writing tokens to the paged cache, and reading it back.  Formats: include/ivfpq.h.
+#include <type_traits>
+
 #include "kv.cuh"
 
 namespace ivfpq {
@@ -12,14 +14,14 @@ constexpr int kThreads = 128;
 // than 2^-22 of it, so it rounds the same unless it lies within 1e-5 of a half; only then is the division done.  Rounding is an addition
 // of 1.5 * 2^23, and four codes are joined as one number below 2^16 in fp32: a division, conversions to integers and shifts for every element
 // took 53 instructions each, 113 us for 21 282 tokens of 8 x 128.
-__device__ __forceinline__ void quantize8(const uint4& in, bool bf16, uint32_t* word, float* scale, float* offset, float* held) {
+template <bool BF>
+__device__ __forceinline__ void quantize8(const uint4& in, uint32_t* word, float* scale, float* offset, float* held) {
     constexpr float kRound = 12582912.f;
     float y[8];
-    unpack8(in, bf16, y);
-    float mn = INFINITY, mx = -INFINITY;
+    unpack8<BF>(in, y);
+    float mn = y[0], mx = y[0];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        y[i] = fminf(fmaxf(y[i], -65504.f), 65504.f);
+    for (int i = 1; i < 8; ++i) {
         mn = fminf(mn, y[i]);
         mx = fmaxf(mx, y[i]);
     }
@@ -29,15 +31,18 @@ __device__ __forceinline__ void quantize8(const uint4& in, bool bf16, uint32_t* 
         mn = fminf(mn, __shfl_xor_sync(m, mn, o));
         mx = fmaxf(mx, __shfl_xor_sync(m, mx, o));
     }
+    // the range is clamped, not the elements: what lies outside ends in code 0 or 15
+    mn = fminf(fmaxf(mn, -65504.f), 65504.f);
+    mx = fminf(fmaxf(mx, -65504.f), 65504.f);
     const float z = __half2float(__float2half_rn(mn));
     const float s = __half2float(__float2half_rn(__fmul_rn(__fsub_rn(mx, z), 1.f / 15.f)));
     const float inv = s > 0.f ? __frcp_rn(s) : 0.f;
     float t[8], off = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float q = __fmul_rn(__fsub_rn(y[i], z), inv);
-        t[i] = __fsub_rn(__fadd_rn(fminf(fmaxf(q, 0.f), 15.f), kRound), kRound);
-        off = fmaxf(off, fabsf(q - t[i]) - (q < 0.f || q > 15.f ? 1e9f : 0.f));
+        const float q = fminf(fmaxf(__fmul_rn(__fsub_rn(y[i], z), inv), 0.f), 15.f);
+        t[i] = __fsub_rn(__fadd_rn(q, kRound), kRound);
+        off = fmaxf(off, fabsf(q - t[i]));
     }
     if (off > 0.49999f) {
 #pragma unroll
@@ -59,8 +64,8 @@ __device__ __forceinline__ void quantize8(const uint4& in, bool bf16, uint32_t* 
 //
 // Work items: request r owns items base(r) .. base(r + 1) - 1 with base(r) = start[r] / page + 2 r, at least as many as
 // the blocks its new tokens can lie in; the item's request is found by binary search, surplus items end at once.
-template <int D>
-__global__ void __launch_bounds__(kThreads) append_kernel(Cache c, Batch b, bool bf16, Rows k, Rows v, int* status) {
+template <int D, bool BF>
+__global__ void __launch_bounds__(kThreads) append_kernel(Cache c, Batch b, Rows k, Rows v, int* status) {
     constexpr int kLanes = D / 8;                 // lanes per token
     constexpr int kRows = kThreads / kLanes;      // tokens per pass
     __shared__ float s_hi[kRows][D], s_lo[kRows][D];
@@ -121,7 +126,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(Cache c, Batch b, bool
                 } else {
                     in[u][0] = *kp;
                 }
-                if (full) unpack8(in[u][0], c.format == IVFPQ_KV_BF16, x);
+                if (full) unpack8<BF>(in[u][0], x);
             } else {
                 uint8_t* rec = record_of(c, page, head, t / kTile);
                 const int tt = t % kTile, g = e / 64;
@@ -129,10 +134,10 @@ __global__ void __launch_bounds__(kThreads) append_kernel(Cache c, Batch b, bool
                 __half* ks = reinterpret_cast<__half*>(rec + key_param(D, tt, g));
                 if (fresh) {
                     float s, z;
-                    quantize8(in[u][0], bf16, kw, &s, &z, x);
+                    quantize8<BF>(in[u][0], kw, &s, &z, x);
                     if (lane % 8 == 0) *reinterpret_cast<__half2*>(ks) = __floats2half2_rn(s, z);
                     float unused[8];
-                    quantize8(in[u][1], bf16, reinterpret_cast<uint32_t*>(rec + value_word(D, tt, e)), &s, &z, unused);
+                    quantize8<BF>(in[u][1], reinterpret_cast<uint32_t*>(rec + value_word(D, tt, e)), &s, &z, unused);
                     if (lane % 8 == 0) {
                         __half* vs = reinterpret_cast<__half*>(rec + value_param(D, tt, g));
                         vs[0] = __float2half_rn(s);
@@ -184,8 +189,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(Cache c, Batch b, bool
 }
 
 // 8 elements of one (token, head) per thread.
-template <int D>
-__global__ void __launch_bounds__(256) read_kernel(Cache c, Batch b, bool bf16, char* k, char* v, int* status) {
+template <int D, bool BF>
+__global__ void __launch_bounds__(256) read_kernel(Cache c, Batch b, char* k, char* v, int* status) {
     const int tok = blockIdx.x * (256 / (D / 8)) + threadIdx.x / (D / 8), head = blockIdx.y, e = threadIdx.x % (D / 8) * 8;
     if (tok >= b.ntok) return;
     const int r = request_of(b, tok);
@@ -209,9 +214,9 @@ __global__ void __launch_bounds__(256) read_kernel(Cache c, Batch b, bool bf16, 
                 const uint32_t vw = *reinterpret_cast<const uint32_t*>(rec + value_word(D, tt, e));
                 float x[8];
                 decode8(kw, __half2float(kp[0]), __half2float(kp[1]), x);
-                wk = pack8(x, bf16);
+                wk = pack8<BF>(x);
                 decode8(vw, __half2float(vp[0]), __half2float(vp[2]), x);
-                wv = pack8(x, bf16);
+                wv = pack8<BF>(x);
             }
         }
     }
@@ -244,23 +249,33 @@ __global__ void __launch_bounds__(256) read_bounds_kernel(Cache c, const int32_t
     lower[i] = lo;
 }
 
+// f(head width, whether bf16) with both known when compiling.
+template <class F>
+void by_type(int d, bool bf16, F f) {
+    auto wide = [&](auto w) {
+        if (bf16) f(w, std::true_type{});
+        else f(w, std::false_type{});
+    };
+    if (d == 64) wide(std::integral_constant<int, 64>{});
+    else if (d == 128) wide(std::integral_constant<int, 128>{});
+    else wide(std::integral_constant<int, 256>{});
+}
+
 }  // namespace
 
 cudaError_t launch_append(const Cache& c, const Batch& b, bool bf16, const Rows& k, const Rows& v, int* status, cudaStream_t st) {
     const int items = b.start ? (b.ntok >> c.page_shift) + 2 * b.nreq : b.nreq;
     const dim3 grid(items, c.nheads);
-    if (c.d == 64) append_kernel<64><<<grid, kThreads, 0, st>>>(c, b, bf16, k, v, status);
-    else if (c.d == 128) append_kernel<128><<<grid, kThreads, 0, st>>>(c, b, bf16, k, v, status);
-    else append_kernel<256><<<grid, kThreads, 0, st>>>(c, b, bf16, k, v, status);
+    auto go = [&](auto d, auto bf) { append_kernel<decltype(d)::value, decltype(bf)::value><<<grid, kThreads, 0, st>>>(c, b, k, v, status); };
+    by_type(c.d, bf16, go);
     return cudaGetLastError();
 }
 
 cudaError_t launch_read(const Cache& c, const Batch& b, bool bf16, char* k, char* v, int* status, cudaStream_t st) {
     const int per = 256 / (c.d / 8);              // tokens of a CTA
     const dim3 grid((b.ntok + per - 1) / per, c.nheads);
-    if (c.d == 64) read_kernel<64><<<grid, 256, 0, st>>>(c, b, bf16, k, v, status);
-    else if (c.d == 128) read_kernel<128><<<grid, 256, 0, st>>>(c, b, bf16, k, v, status);
-    else read_kernel<256><<<grid, 256, 0, st>>>(c, b, bf16, k, v, status);
+    auto go = [&](auto d, auto bf) { read_kernel<decltype(d)::value, decltype(bf)::value><<<grid, 256, 0, st>>>(c, b, k, v, status); };
+    by_type(c.d, bf16, go);
     return cudaGetLastError();
 }
 
