@@ -92,7 +92,8 @@ __device__ __forceinline__ bool tile_of(const AttendArgs& a, const Plan& p, int 
     return true;
 }
 
-template <int FMT, int D, int NT, bool LIST>
+// P16: 4-bit pages of 16 tokens, whose records of a stage lie apart.
+template <int FMT, int D, int NT, bool LIST, bool P16>
 __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, NT>::kMinCtas)) attend_kernel(AttendArgs a, Plan plan) {
     using S = Shape<FMT, D, NT>;
     constexpr bool kInt4 = S::kInt4;
@@ -277,81 +278,104 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
         const int vlen = LIST ? a.nselect << c.page_shift : lim_hi;
         const int32_t* list = LIST ? a.blocks + ((int64_t)tl.tok0 * c.nheads + head) * a.nselect : nullptr;
 
-        // ---- 16-key pieces of the warp: piece s covers (virtual) keys (u0 + s / 2) 128 + 32 warp + 16 (s % 2) ----
-        const int nsub = (u1 - u0) * run * 2, nstage = nsub / S::kSubs;      // those past the last key are passed over
-        const char *k_cur = nullptr, *k_nxt = nullptr, *v_cur = nullptr, *v_nxt = nullptr;   // where piece (batch, lane) is held
-        int pos_cur = 0, pos_nxt = 0;         // and the position of its first key
-        auto look = [&](int s, const char** kp, const char** vp, int* pos) {
-            *kp = nullptr;
-            *pos = lim_hi;                    // no key: masked throughout
-            if (s >= nsub || (kInt4 && s_dead[warp])) return;
-            const int vk = (u0 * run + (s >> 1)) * kUnit + warp * 32 + (s & 1) * 16;
-            if (vk >= vlen) return;
+        // ---- stages of the warp: stage i covers 32 (virtual) keys from (u0 run + i) kUnit + 32 warp on (16-bit formats:
+        //      16, two stages to 32).  Each lane looks one stage up, 32 stages ahead of their use. ----
+        const int nstage = (u1 - u0) * run * (32 / S::kStageKeys);      // those past the last key are passed over
+        struct Look {
+            const char *k, *v;                // where the stage's keys and values are held; 4-bit pages of 16: v is the second record
+            int pos, pos2;                    // position of the first key, lim_hi if there is none; of the second record
+        };
+        auto piece = [&](int vk, const char** kp, const char** vp) -> int {
+            if (vk >= vlen) return lim_hi;
             int blk = vk >> c.page_shift;
             if (LIST) {
                 blk = list[blk];
-                if (blk < 0 || (int64_t)blk << c.page_shift >= lim_hi) return;
+                if (blk < 0 || (int64_t)blk << c.page_shift >= lim_hi) return lim_hi;
             }
-            const int tk = vk & (c.page - 1);
-            const int at0 = (blk << c.page_shift) + tk;
-            if (at0 >= lim_hi) return;
+            const int tk = vk & (c.page - 1), at0 = (blk << c.page_shift) + tk;
+            if (at0 >= lim_hi) return lim_hi;
             const int pg = page_of(a.b, c, tl.r, blk, status);
-            if (pg < 0) return;
-            *pos = at0;
+            if (pg < 0) return lim_hi;
             if (kInt4) {
                 *kp = reinterpret_cast<const char*>(record_of(c, pg, head, tk >> 4));
             } else {
                 *kp = c.k + 2 * (pg * c.ks[0] + head * c.ks[1] + tk * c.ks[2]);
                 *vp = c.v + 2 * (pg * c.vs[0] + head * c.vs[1] + tk * c.vs[2]);
             }
+            return at0;
         };
-        look(lane, &k_cur, &v_cur, &pos_cur);
+        auto look = [&](int st) -> Look {
+            Look x{nullptr, nullptr, lim_hi, lim_hi};
+            if (st >= nstage || (kInt4 && s_dead[warp])) return x;
+            if (kInt4) {
+                const int vk = (u0 * run + st) * kUnit + warp * 32;
+                x.pos = piece(vk, &x.k, nullptr);
+                x.pos2 = P16 ? piece(vk + 16, &x.v, nullptr) : x.pos + 16;
+            } else {
+                x.pos = piece((u0 * run + (st >> 1)) * kUnit + warp * 32 + (st & 1) * 16, &x.k, &x.v);
+            }
+            return x;
+        };
+        Look cur = look(lane), nxt;
         auto issue = [&](int st) {            // stage st of the segment into the next slot
             if (st < nstage) {
-                const int s0 = st * S::kSubs, l0 = s0 & 31;
-                if (s0 && l0 == 0) {
-                    k_cur = k_nxt;
-                    v_cur = v_nxt;
-                    pos_cur = pos_nxt;
-                    look(s0 + 32 + lane, &k_nxt, &v_nxt, &pos_nxt);
+                const int l0 = st & 31;
+                if (st && l0 == 0) {
+                    cur = nxt;
+                    nxt = look(st + 32 + lane);
                 }
                 const uint32_t dst = ring_u + put * S::kStageBytes;
                 if (kInt4) {
-                    // pages of 32 tokens and more: the second piece follows the first, and one lane knows all
-                    int second = pos_cur + 16;
-                    const char* kp2 = nullptr;
-                    if (c.page == 16) {
-                        second = __shfl_down_sync(0xffffffffu, pos_cur, 1);
-                        kp2 = reinterpret_cast<const char*>(__shfl_down_sync(0xffffffffu, reinterpret_cast<unsigned long long>(k_cur), 1));
-                    }
+                    // the lane that knows the stage starts its copy: the two records lie together but for pages of 16
                     if (lane == l0) {
                         const uint32_t bar = smem_u32(&s_bar[warp][put]);
-                        const uint32_t n0 = pos_cur < lim_hi ? 18 * D : 0, n1 = second < lim_hi ? 18 * D : 0;
-                        *reinterpret_cast<int2*>(s_info[warp][put]) = make_int2(pos_cur, second);
-                        if (n0 + n1) mbar_expect(bar, n0 + n1);
-                        else mbar_arrive(bar);
-                        if (!kp2) {
-                            if (n0) bulk_load(dst, k_cur, n0 + n1, bar);
+                        const uint32_t n0 = cur.pos < lim_hi ? 18 * D : 0, n1 = cur.pos2 < lim_hi ? 18 * D : 0;
+                        if (P16) {
+                            *reinterpret_cast<int2*>(s_info[warp][put]) = make_int2(cur.pos, cur.pos2);
+                            if (n0 + n1) mbar_expect(bar, n0 + n1);
+                            else mbar_arrive(bar);
+                            if (n0) bulk_load(dst, cur.k, n0, bar);
+                            if (n1) bulk_load(dst + 18 * D, cur.v, n1, bar);
                         } else {
-                            if (n0) bulk_load(dst, k_cur, n0, bar);
-                            if (n1) bulk_load(dst + 18 * D, kp2, n1, bar);
+                            s_info[warp][put][0] = cur.pos;
+                            if (n0) {
+                                mbar_expect(bar, n0 + n1);
+                                bulk_load(dst, cur.k, n0 + n1, bar);
+                            } else {
+                                mbar_arrive(bar);
+                            }
                         }
                     }
                 } else {
-                    const char* kp = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(k_cur), l0));
-                    const char* vp = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(v_cur), l0));
-                    const int pos = __shfl_sync(0xffffffffu, pos_cur, l0);
+                    const char* kp = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(cur.k), l0));
+                    const char* vp = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(cur.v), l0));
+                    const int pos = __shfl_sync(0xffffffffu, cur.pos, l0);
                     if (lane == 0) s_info[warp][put][0] = pos;
                     if (kp) {
-                        constexpr int CH = D / 8;                         // 16-byte chunks of a row
+                        constexpr int CH = D / 8, RS = 32 / CH > 0 ? 32 / CH : 1;      // 16-byte chunks of a row; rows of a pass
+                        constexpr int PASSES = 16 * CH / 32;
+                        const int row0 = lane / CH, ch0 = lane % CH;
+                        if (pos + 16 <= lim_hi) {
+                            const char *kq = kp + 2 * (row0 * c.ks[2] + ch0 * 8), *vq = vp + 2 * (row0 * c.vs[2] + ch0 * 8);
 #pragma unroll
-                        for (int i = 0; i < 16 * CH / 32; ++i) {
-                            const int x = i * 32 + lane, row = x / CH, ch = x % CH;
-                            const uint32_t o = row * (2 * D) + ((ch ^ (row & 7)) * 16);
-                            const bool real = pos + row < lim_hi;
-                            const int rr = real ? row : 0;
-                            cp_async16(dst + o, kp + 2 * (rr * c.ks[2] + ch * 8), real);
-                            cp_async16(dst + 16 * D * 2 + o, vp + 2 * (rr * c.vs[2] + ch * 8), real);
+                            for (int i = 0; i < PASSES; ++i) {
+                                // D = 256: a row is 32 chunks, one pass; else RS rows a pass
+                                const int row = row0 + i * RS;
+                                const uint32_t o = row * (2 * D) + ((ch0 ^ (row & 7)) * 16);
+                                cp_async16(dst + o, kq, true);
+                                cp_async16(dst + 16 * D * 2 + o, vq, true);
+                                kq += 2 * RS * c.ks[2];
+                                vq += 2 * RS * c.vs[2];
+                            }
+                        } else {
+                            for (int i = 0; i < PASSES; ++i) {
+                                const int row = row0 + i * RS;
+                                const uint32_t o = row * (2 * D) + ((ch0 ^ (row & 7)) * 16);
+                                const bool real = pos + row < lim_hi;
+                                const int rr = real ? row : 0;
+                                cp_async16(dst + o, kp + 2 * (rr * c.ks[2] + ch0 * 8), real);
+                                cp_async16(dst + 16 * D * 2 + o, vp + 2 * (rr * c.vs[2] + ch0 * 8), real);
+                            }
                         }
                     }
                 }
@@ -365,7 +389,7 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < S::kStages - 1; ++i) issue(i);
-        look(lane + 32, &k_nxt, &v_nxt, &pos_nxt);
+        nxt = look(lane + 32);
 
         // ---- queries ----
         uint32_t qf[NT][KSTEPS][2];
@@ -478,13 +502,9 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
                 __syncwarp();
             }
             int pos[S::kSubs];
-            bool none = true;
-#pragma unroll
-            for (int i = 0; i < S::kSubs; ++i) {
-                pos[i] = s_info[warp][slot][i];
-                none = none && pos[i] >= lim_hi;
-            }
-            if (none) continue;               // uniform over the warp
+            pos[0] = s_info[warp][slot][0];
+            if (S::kSubs == 2) pos[S::kSubs - 1] = P16 ? s_info[warp][slot][1] : pos[0] + 16;
+            if (pos[0] >= lim_hi && (!P16 || pos[S::kSubs - 1] >= lim_hi)) continue;      // uniform over the warp
             const char* buf = ring + slot * S::kStageBytes;
             const uint32_t buf_u = ring_u + slot * S::kStageBytes;
             float p[S::kSubs][NT][4];
@@ -549,7 +569,7 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
                     }
                 }
             }
-            if (max(pos[0], pos[S::kSubs - 1]) + 16 > lim_lo) {
+            if ((P16 ? max(pos[0], pos[S::kSubs - 1]) : pos[S::kSubs - 1]) + 16 > lim_lo) {
 #pragma unroll
                 for (int i = 0; i < S::kSubs; ++i)
 #pragma unroll
@@ -838,11 +858,11 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
     }
 }
 
-template <int FMT, int D, int NT, bool LIST>
+template <int FMT, int D, int NT, bool LIST, bool P16>
 cudaError_t run(const AttendArgs& a, int sms, cudaStream_t st) {
     using S = Shape<FMT, D, NT>;
     constexpr int R = S::kRows;
-    auto kernel = attend_kernel<FMT, D, NT, LIST>;
+    auto kernel = attend_kernel<FMT, D, NT, LIST, P16>;
     static int known[64];                     // per instance and device: CTAs an SM holds
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
@@ -882,8 +902,13 @@ cudaError_t pick_rows(const AttendArgs& a, int sms, cudaStream_t st) {
     const bool list = a.blocks != nullptr;
     // rows that can share a kv head: one token's query heads, or those of several tokens of a request
     const bool wide = a.group > 8 || (!list && a.b.start != nullptr);
-    if (list) return wide ? run<FMT, D, 2, true>(a, sms, st) : run<FMT, D, 1, true>(a, sms, st);
-    return wide ? run<FMT, D, 2, false>(a, sms, st) : run<FMT, D, 1, false>(a, sms, st);
+    if (FMT == IVFPQ_KV_INT4 && a.c.page == 16) {
+        constexpr bool P = FMT == IVFPQ_KV_INT4;
+        if (list) return wide ? run<FMT, D, 2, true, P>(a, sms, st) : run<FMT, D, 1, true, P>(a, sms, st);
+        return wide ? run<FMT, D, 2, false, P>(a, sms, st) : run<FMT, D, 1, false, P>(a, sms, st);
+    }
+    if (list) return wide ? run<FMT, D, 2, true, false>(a, sms, st) : run<FMT, D, 1, true, false>(a, sms, st);
+    return wide ? run<FMT, D, 2, false, false>(a, sms, st) : run<FMT, D, 1, false, false>(a, sms, st);
 }
 
 template <int FMT>
