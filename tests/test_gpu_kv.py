@@ -520,3 +520,12 @@ def test_selecting_every_block_is_the_whole_cache():
         whole = lib.ivfpq_kv_attend(s.cache, s.batch, s.q)
         blocks = lib.ivfpq_kv_select(s.cache, s.batch, s.q, 32)
         assert torch.allclose(lib.ivfpq_kv_attend(s.cache, s.batch, s.q, blocks=blocks).float(), whole.float(), atol=2e-2, rtol=2e-2)
+
+
+@pytest.mark.parametrize("bits", [4, 16])
+def test_the_curve_of_kept_attention(bits):
+    from paper_2312_01712_b200 import kv_curve
+    rows = kv_curve.curve([4, 12, 40], context=2400, nreq=3, hkv=2, page=64, bits=bits)
+    kept, error = [r["kept_attention"] for r in rows], [r["rel_error"] for r in rows]
+    assert kept == sorted(kept) and kept[0] > 0.02 and abs(kept[-1] - 1) < 1e-3      # 38 blocks: the last row lists them all
+    assert error[0] > error[1] > error[2] and error[2] < 1e-2
