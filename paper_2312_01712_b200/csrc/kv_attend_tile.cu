@@ -16,6 +16,7 @@
 // only.  (Looking at every value as it came cost 18 of 211 us.)
 //
 // Every wait is bounded: one that runs out raises the status flag, all roles leave, and tensor memory is freed.
+#include <cuda.h>
 #include <type_traits>
 
 #include "kv_mma.cuh"
@@ -41,6 +42,7 @@ struct TileShape {
 
 struct TilePlan {
     int32_t tokens;          // of a tile
+    int32_t maps;            // 1: the cache's strides have tensor maps
     int32_t list_cap;        // entries of the union
 };
 
@@ -109,6 +111,12 @@ __device__ __forceinline__ bool elect_one() {
     asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(p));
     return p;
 }
+// 64 elements of width x some tokens of one head and page.
+__device__ __forceinline__ void tensor_load(uint32_t dst, const CUtensorMap* map, int x, int token, int head, int page, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(token), "r"(head), "r"(page)
+                 : "memory");
+}
 // Descriptor of a 128-byte swizzled tile: groups of 8 rows of 128 bytes, 1024 bytes apart; `lead` is the distance of 64-element slabs where the
 // tile's rows run along the summed axis (values), unused otherwise.
 __device__ __forceinline__ uint64_t tile_desc(uint32_t addr, uint32_t lead) {
@@ -116,7 +124,8 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t addr, uint32_t lead) {
 }
 
 template <bool BF, int D>
-__global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_kernel(AttendArgs a, TilePlan p) {
+__global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas))
+attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, AttendArgs a, TilePlan p) {
     using S = TileShape<D>;
     constexpr int CH = D / 8;
     extern __shared__ __align__(1024) unsigned char dyn[];
@@ -233,10 +242,33 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
             }
             const int64_t s0 = V ? c.vs[0] : c.ks[0], s1 = V ? c.vs[1] : c.ks[1], s2 = V ? c.vs[2] : c.ks[2];
             const char* src0 = (V ? c.v : c.k) + 2 * (head * s1 + ch * 8);
-            for (int st = 0; st < nstep; ++st) {
+            int st = 0;
+            for (; st < nstep; ++st) {
                 const int slot = st % kStages;
                 if (st >= kStages && !wait_bar<true>(V ? &sh->v_empty[slot] : &sh->k_empty[slot], ((st / kStages) & 1) ^ 1, sh, status)) break;
                 const uint32_t dst = kv_s + slot * 2 * S::kKV + (V ? S::kKV : 0) + (ch / 8) * (kKeys * 128);
+                unsigned long long* full = V ? &sh->v_full[slot] : &sh->k_full[slot];
+                // All of the step's keys held: tensor copies, started by one lane (a copy per 64 elements of width and entry).  The last block of the
+                // tile's reach goes row by row, with zeros past its last key.
+                const int e0 = st * pieces, e1 = pieces == 1 ? st >> half_shift : e0 + pieces - 1;
+                const int off = (st & (halves - 1)) * kKeys;
+                const bool whole = p.maps && e1 < total && (s_list[e1].x << c.page_shift) + (pieces == 1 ? off + kKeys : piece) <= lim_hi;
+                if (whole) {
+                    const uint32_t bar = smem_u32(full);
+                    if (t == 0) {
+                        mbar_expect(bar, S::kKV);
+                        const uint32_t tile = kv_s + slot * 2 * S::kKV + (V ? S::kKV : 0);
+                        for (int i = 0; i < pieces; ++i) {
+                            const int page = s_list[pieces == 1 ? e1 : e0 + i].y;
+#pragma unroll
+                            for (int x = 0; x < D / 64; ++x)
+                                tensor_load(tile + x * (kKeys * 128) + i * piece * 128, V ? &map_v : &map_k, x * 64, off, head, page, bar);
+                        }
+                    } else {
+                        mbar_arrive(bar);
+                    }
+                    continue;
+                }
                 if (pieces == 1) {
                     // one entry: rows a fixed distance apart
                     const int2 en = s_list[st >> half_shift];
@@ -258,9 +290,14 @@ __global__ void __launch_bounds__(kThreads, (TileShape<D>::kCtas)) attend_tile_k
                 cp_async_commit();
                 cp_async_wait<0>();
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                mbar_arrive(smem_u32(V ? &sh->v_full[slot] : &sh->k_full[slot]));
+                mbar_arrive(smem_u32(full));
             }
             cp_async_wait<0>();
+            // the products have waited for every copy, unless somebody gave up: then none may be on its way when the CTA ends
+            if (sh->abort && t == 0)
+                for (int i = max(st - kStages, 0); i < st; ++i)
+                    for (unsigned k = 0; k < kSpins; ++k)
+                        if (mbar_try(smem_u32(V ? &sh->v_full[i % kStages] : &sh->k_full[i % kStages]), (i / kStages) & 1)) break;
         };
         if (values) run(std::true_type{});
         else run(std::false_type{});
@@ -469,6 +506,27 @@ size_t tile_smem(const AttendArgs& a, TilePlan* p) {
     return 1024 + (size_t)TileShape<D>::kBytes + sizeof(TileShared) + (size_t)a.b.max_blocks * 8 + (size_t)p->list_cap * 8;
 }
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The cache's keys or values as [page][head][token][d] with boxes of 64 elements x the tokens of an entry; false where the strides have no such map.
+bool make_map(CUtensorMap* map, const Cache& c, char* base, const int64_t (&stride)[3]) {
+    static EncodeTiledFn fn = []() -> EncodeTiledFn {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) return nullptr;
+        return reinterpret_cast<EncodeTiledFn>(p);
+    }();
+    if (!fn) return false;
+    for (int i = 0; i < 3; ++i)
+        if (stride[i] <= 0) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)c.d, (cuuint64_t)c.page, (cuuint64_t)c.nheads, (cuuint64_t)c.npages};
+    const cuuint64_t strides[3] = {(cuuint64_t)stride[2] * 2, (cuuint64_t)stride[1] * 2, (cuuint64_t)stride[0] * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)(c.page < kKeys ? c.page : kKeys), 1, 1}, one[4] = {1, 1, 1, 1};
+    return fn(map, c.format == IVFPQ_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dims, strides, box, one,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <bool BF, int D>
 cudaError_t run(const AttendArgs& a, cudaStream_t st) {
     TilePlan p{};
@@ -476,7 +534,9 @@ cudaError_t run(const AttendArgs& a, cudaStream_t st) {
     auto kernel = attend_tile_kernel<BF, D>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    kernel<<<dim3(a.b.ntok / p.tokens + a.b.nreq, a.c.nheads), kThreads, smem, st>>>(a, p);
+    alignas(64) CUtensorMap map_k{}, map_v{};
+    p.maps = make_map(&map_k, a.c, a.c.k, a.c.ks) && make_map(&map_v, a.c, a.c.v, a.c.vs);
+    kernel<<<dim3(a.b.ntok / p.tokens + a.b.nreq, a.c.nheads), kThreads, smem, st>>>(map_k, map_v, a, p);
     return cudaGetLastError();
 }
 
