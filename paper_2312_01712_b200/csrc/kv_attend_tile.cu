@@ -94,8 +94,8 @@ __device__ __forceinline__ void tc_load32(uint32_t at, uint32_t (&v)[32]) {
                    "=r"(v[31])
                  : "r"(at)
                  : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void tc_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_store32(uint32_t at, const uint32_t (&v)[32]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
                  "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
@@ -360,18 +360,20 @@ attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
         const float fscale = fmaxf(a.scale, 1e-30f) * kLog2e;      // a masked product is -infinity and has to stay it
         // keys of a step that the row sees, as bits; found for the next step while this one's P is on its way
+        const uint32_t* mask_word = reinterpret_cast<const uint32_t*>(s_mask) + (j >> 5 & 1);      // the half of a mask that holds the token
+        const uint32_t mask_bit = 1u << (j & 31);
         auto seen_of = [&](int st) -> unsigned long long {
             if (row >= nrows || st >= nstep) return 0ull;
             if (pieces == 1) {
                 const int e = st >> half_shift;
-                if (!(s_mask[e] >> j & 1ull)) return 0ull;
                 const int v = lim - ((s_list[e].x << c.page_shift) + (st & (halves - 1)) * kKeys);
-                return v >= kKeys ? ~0ull : v <= 0 ? 0ull : (1ull << v) - 1ull;
+                if (!(mask_word[2 * e] & mask_bit) || v <= 0) return 0ull;
+                return v >= kKeys ? ~0ull : (1ull << v) - 1ull;
             }
             unsigned long long bits = 0ull;
             for (int i = 0; i < pieces; ++i) {
                 const int e = st * pieces + i;
-                if (e >= total || !(s_mask[e] >> j & 1ull)) continue;
+                if (e >= total || !(mask_word[2 * e] & mask_bit)) continue;
                 const int v = min(max(lim - (s_list[e].x << c.page_shift), 0), piece);
                 bits |= ((1ull << v) - 1ull) << (i * piece);
             }
@@ -398,6 +400,7 @@ attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 uint32_t v[2][32];
                 tc_load32(lanes + (st & 1) * kKeys, v[0]);
                 tc_load32(lanes + (st & 1) * kKeys + 32, v[1]);
+                tc_wait_load();
                 if (partly) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
@@ -442,6 +445,7 @@ attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 for (int cc = 0; cc < D; cc += 32) {
                     uint32_t x[32];
                     tc_load32(lanes + 2 * kKeys + cc, x);
+                    tc_wait_load();
 #pragma unroll
                     for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * raise);
                     tc_store32(lanes + 2 * kKeys + cc, x);
@@ -462,7 +466,10 @@ attend_tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         bool finite = true;
         for (int cc = 0; cc < D; cc += 32) {
             uint32_t x[32];
-            if (nstep > 0) tc_load32(lanes + 2 * kKeys + cc, x);
+            if (nstep > 0) {
+                tc_load32(lanes + 2 * kKeys + cc, x);
+                tc_wait_load();
+            }
             if (row < nrows) {
                 if (nstep > 0) {
 #pragma unroll
