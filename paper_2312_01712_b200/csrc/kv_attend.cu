@@ -278,6 +278,30 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
         const int vlen = LIST ? a.nselect << c.page_shift : lim_hi;
         const int32_t* list = LIST ? a.blocks + ((int64_t)tl.tok0 * c.nheads + head) * a.nselect : nullptr;
 
+        // ---- queries: requested before anything that depends on the block table ----
+        uint4 raw[NT][kInt4 ? G : 1][2];      // 4-bit: the lane's words (group, half): elements 64 group + 16 lc + 8 half + 0..7
+        uint32_t qf[NT][KSTEPS][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = tl.row0 + nt * 8 + lr;
+            const bool real = row < tl.nrows;
+            const int j = real && tl.n > 1 ? row / a.group : 0, g = real ? row - j * a.group : 0;
+            const char* qp = a.q.p + 2 * ((int64_t)(tl.tok0 + j) * a.q.ts + (int64_t)(head * a.group + g) * a.q.hs);
+            if (kInt4) {
+#pragma unroll
+                for (int gr = 0; gr < G; ++gr)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        raw[nt][gr][h] = real ? *reinterpret_cast<const uint4*>(qp + 2 * (64 * gr + 16 * lc + 8 * h)) : make_uint4(0, 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int s = 0; s < KSTEPS; ++s) {
+                    qf[nt][s][0] = real ? *reinterpret_cast<const uint32_t*>(qp + 2 * (16 * s + 2 * lc)) : 0u;
+                    qf[nt][s][1] = real ? *reinterpret_cast<const uint32_t*>(qp + 2 * (16 * s + 8 + 2 * lc)) : 0u;
+                }
+            }
+        }
+
         // ---- stages of the warp: stage i covers 32 (virtual) keys from (u0 run + i) kUnit + 32 warp on (16-bit formats:
         //      16, two stages to 32).  Each lane looks one stage up, 32 stages ahead of their use. ----
         const int nstage = (u1 - u0) * run * (32 / S::kStageKeys);      // those past the last key are passed over
@@ -391,8 +415,7 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
         for (int i = 0; i < S::kStages - 1; ++i) issue(i);
         nxt = look(lane + 32);
 
-        // ---- queries ----
-        uint32_t qf[NT][KSTEPS][2];
+        // ---- queries as operands ----
         float qs[NT][kInt4 ? G : 1][2];       // 4-bit: sums of a column's query elements over each group, times 2^-24
         // factor from products to base-2 logits, positive: a negative scale turns the queries' signs, zero becomes tiny (a masked
         // product is -infinity and has to stay it)
@@ -402,57 +425,47 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
         int lim[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int row = tl.row0 + nt * 8 + lr;
-            const bool real = row < tl.nrows;
-            const int j = real ? row / a.group : 0, g = real ? row % a.group : 0;
-            const char* qp = a.q.p + 2 * ((int64_t)(tl.tok0 + j) * a.q.ts + (int64_t)(head * a.group + g) * a.q.hs);
             if (!kInt4) {
 #pragma unroll
                 for (int s = 0; s < KSTEPS; ++s) {
-                    qf[nt][s][0] = real ? *reinterpret_cast<const uint32_t*>(qp + 2 * (16 * s + 2 * lc)) ^ flip : 0u;
-                    qf[nt][s][1] = real ? *reinterpret_cast<const uint32_t*>(qp + 2 * (16 * s + 8 + 2 * lc)) ^ flip : 0u;
+                    qf[nt][s][0] ^= flip;
+                    qf[nt][s][1] ^= flip;
                 }
                 cf[nt][0] = cf[nt][1] = fscale;
             } else {
-                // the lane's words (group, half): elements 64 group + 16 lc + 8 half + 0..7, scaled by a power of two to just below 2^15
-                uint4 raw[G][2];
-                float top = 0.f;
+                // scaled by a power of two to just below 2^15
+                float x[G][2][8], top = 0.f;
+                if (a.bf16) {
 #pragma unroll
-                for (int gr = 0; gr < G; ++gr)
+                    for (int i = 0; i < 2 * G; ++i) unpack8<true>(raw[nt][i / 2][i % 2], x[i / 2][i % 2]);
+                } else {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        raw[gr][h] = real ? *reinterpret_cast<const uint4*>(qp + 2 * (64 * gr + 16 * lc + 8 * h)) : make_uint4(0, 0, 0, 0);
-                        float x[8];
-                        unpack8(raw[gr][h], a.bf16, x);
+                    for (int i = 0; i < 2 * G; ++i) unpack8<false>(raw[nt][i / 2][i % 2], x[i / 2][i % 2]);
+                }
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
-                    }
+                for (int i = 0; i < 16 * G; ++i) top = fmaxf(top, fabsf(x[i / 16][i / 8 % 2][i % 8]));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 const int ex = top > 0.f ? min(max(14 - ((int)(__float_as_uint(top) >> 23) - 127), -100), 100) : 0;
-                const float up = __uint_as_float((uint32_t)(127 + ex) << 23 | (flip & 0x80000000u));
+                const float up = __uint_as_float((uint32_t)(127 + ex) << 23 | (flip & 0x80000000u)), up16 = up * 0.0625f;
                 const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
 #pragma unroll
                 for (int gr = 0; gr < G; ++gr) {
                     float sum = 0.f;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        float x[8];
-                        unpack8(raw[gr][h], a.bf16, x);
+                        const float* y = x[gr][h];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            x[i] *= up;
-                            sum += x[i];
-                        }
+                        for (int i = 0; i < 8; ++i) sum += y[i];
                         const int s = (gr * 2 + h) * 2;
-                        qf[nt][s][0] = pack2<false>(x[0], x[4]);
-                        qf[nt][s][1] = pack2<false>(x[1] * 0.0625f, x[5] * 0.0625f);
-                        qf[nt][s + 1][0] = pack2<false>(x[2], x[6]);
-                        qf[nt][s + 1][1] = pack2<false>(x[3] * 0.0625f, x[7] * 0.0625f);
+                        qf[nt][s][0] = pack2<false>(y[0] * up, y[4] * up);
+                        qf[nt][s][1] = pack2<false>(y[1] * up16, y[5] * up16);
+                        qf[nt][s + 1][0] = pack2<false>(y[2] * up, y[6] * up);
+                        qf[nt][s + 1][1] = pack2<false>(y[3] * up16, y[7] * up16);
                     }
                     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                    sum *= 5.9604644775390625e-08f;                       // 2^-24
+                    sum *= up * 5.9604644775390625e-08f;                  // 2^-24
                     qs[nt][gr][0] = __shfl_sync(0xffffffffu, sum, lc * 8);
                     qs[nt][gr][1] = __shfl_sync(0xffffffffu, sum, lc * 8 + 4);
                 }
@@ -463,7 +476,7 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
 #pragma unroll
             for (int j2 = 0; j2 < 2; ++j2) {
                 const int col = tl.row0 + nt * 8 + lc * 2 + j2;
-                lim[nt][j2] = col < tl.nrows ? tl.limit(col, a.group) : lim_hi;
+                lim[nt][j2] = tl.n > 1 && col < tl.nrows ? tl.limit(col, a.group) : lim_hi;
             }
         }
 
