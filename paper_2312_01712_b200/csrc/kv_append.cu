@@ -11,7 +11,7 @@ constexpr int kThreads = 128;
 
 // Codes of 8 consecutive elements of a group of 64, spread over 8 neighbouring lanes, to *word; scale, offset and the held values.
 // The code is rint of the correctly rounded quotient (x - z) / s.  A product with the reciprocal differs from the quotient by less
-// than 2^-22 of it, so it rounds the same unless it lies within 1e-5 of a half; only then is the division done.  Rounding is an addition
+// than 2^-21 of it, so it rounds the same unless it lies within 1e-5 of a half; only then is the division done.  Rounding is an addition
 // of 1.5 * 2^23, and four codes are joined as one number below 2^16 in fp32: a division, conversions to integers and shifts for every element
 // took 53 instructions each, 113 us for 21 282 tokens of 8 x 128.
 template <bool BF>
@@ -36,13 +36,14 @@ __device__ __forceinline__ void quantize8(const uint4& in, uint32_t* word, float
     mx = fminf(fmaxf(mx, -65504.f), 65504.f);
     const float z = __half2float(__float2half_rn(mn));
     const float s = __half2float(__float2half_rn(__fmul_rn(__fsub_rn(mx, z), 1.f / 15.f)));
-    const float inv = s > 0.f ? __frcp_rn(s) : 0.f;
+    // a fifteenth of the quotient, so that the clamp to 0..15 is the multiplication's saturation
+    const float inv = s > 0.f ? __fmul_rn(__frcp_rn(s), 1.f / 15.f) : 0.f;
     float t[8], off = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float q = fminf(fmaxf(__fmul_rn(__fsub_rn(y[i], z), inv), 0.f), 15.f);
-        t[i] = __fsub_rn(__fadd_rn(q, kRound), kRound);
-        off = fmaxf(off, fabsf(q - t[i]));
+        const float q = __saturatef(__fmul_rn(__fsub_rn(y[i], z), inv));
+        t[i] = __fsub_rn(__fmaf_rn(q, 15.f, kRound), kRound);
+        off = fmaxf(off, fabsf(__fmaf_rn(q, 15.f, -t[i])));
     }
     if (off > 0.49999f) {
 #pragma unroll
@@ -57,7 +58,7 @@ __device__ __forceinline__ void quantize8(const uint4& in, uint32_t* word, float
     *offset = z;
 }
 
-// One CTA writes the new tokens of one (request, block, kv head).  A token's d elements are spread over d / 8
+// One CTA writes the new keys, or the new values, of one (request, block, kv head).  A token's d elements are spread over d / 8
 // lanes, 8 consecutive elements (16 bytes in, one 32-bit word of codes out) each, so that a group of 64 is 8
 // neighbouring lanes and its extrema are three shuffles.  When the block becomes full its bounds follow from the held
 // values: those of the tokens just written come from registers, older ones are read back from the cache.
@@ -91,7 +92,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(Cache c, Batch b, Rows
     if (p0 >= len) return;
     const int page = page_of(b, c, r, blk, status);
     if (page < 0) return;
-    const bool full = c.bounds && p0 + c.page <= len;
+    const bool values = blockIdx.z;
+    const bool full = !values && c.bounds && p0 + c.page <= len;
     const int lane = threadIdx.x % kLanes, row = threadIdx.x / kLanes, e = lane * 8;
     const int t_begin = full ? 0 : max(first - p0, 0), t_end = min(c.page, len - p0);
     float hi[8], lo[8];
@@ -100,59 +102,50 @@ __global__ void __launch_bounds__(kThreads) append_kernel(Cache c, Batch b, Rows
         hi[i] = -INFINITY;
         lo[i] = INFINITY;
     }
-    // K and V of two passes are loaded before either is used
-    for (int t0 = t_begin; t0 < t_end; t0 += 2 * kRows) {
-        uint4 in[2][2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int t = t0 + u * kRows + row;
-            if (t >= t_end || p0 + t < first) continue;
-            const int64_t src = tok.x + (p0 + t - (len - tok.y));
-            in[u][0] = __ldg(reinterpret_cast<const uint4*>(k.p + 2 * (src * k.ts + head * k.hs + e)));
-            in[u][1] = __ldg(reinterpret_cast<const uint4*>(v.p + 2 * (src * v.ts + head * v.hs + e)));
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int t = t0 + u * kRows + row;
-            if (t >= t_end) continue;             // whole groups of kLanes lanes
-            const bool fresh = p0 + t >= first;
-            float x[8];
-            if (c.format != IVFPQ_KV_INT4) {
-                uint4* kp = reinterpret_cast<uint4*>(c.k + 2 * (page * c.ks[0] + head * c.ks[1] + t * c.ks[2] + e));
-                uint4* vp = reinterpret_cast<uint4*>(c.v + 2 * (page * c.vs[0] + head * c.vs[1] + t * c.vs[2] + e));
-                if (fresh) {
-                    *kp = in[u][0];
-                    *vp = in[u][1];
-                } else {
-                    in[u][0] = *kp;
-                }
-                if (full) unpack8<BF>(in[u][0], x);
-            } else {
-                uint8_t* rec = record_of(c, page, head, t / kTile);
-                const int tt = t % kTile, g = e / 64;
-                uint32_t* kw = reinterpret_cast<uint32_t*>(rec + key_word(D, tt, e));
-                __half* ks = reinterpret_cast<__half*>(rec + key_param(D, tt, g));
-                if (fresh) {
-                    float s, z;
-                    quantize8<BF>(in[u][0], kw, &s, &z, x);
-                    if (lane % 8 == 0) *reinterpret_cast<__half2*>(ks) = __floats2half2_rn(s, z);
-                    float unused[8];
-                    quantize8<BF>(in[u][1], reinterpret_cast<uint32_t*>(rec + value_word(D, tt, e)), &s, &z, unused);
-                    if (lane % 8 == 0) {
-                        __half* vs = reinterpret_cast<__half*>(rec + value_param(D, tt, g));
-                        vs[0] = __float2half_rn(s);
-                        vs[2] = __float2half_rn(z);
+    const Rows& in = values ? v : k;
+    const char* src = in.p + 2 * ((int64_t)(tok.x + p0 - (len - tok.y)) * in.ts + (int64_t)head * in.hs + e);      // of token 0 of the block
+    auto load = [&](int t) -> uint4 {             // the next pass's elements, while this one's are worked on
+        return t < t_end && p0 + t >= first ? __ldg(reinterpret_cast<const uint4*>(src + 2 * t * in.ts)) : make_uint4(0, 0, 0, 0);
+    };
+    uint4 next = load(t_begin + row);
+    for (int t0 = t_begin; t0 < t_end; t0 += kRows) {
+        const int t = t0 + row;
+        uint4 now = next;
+        next = load(t + kRows);
+        if (t >= t_end) continue;                 // whole groups of kLanes lanes
+        const bool fresh = p0 + t >= first;
+        float x[8];
+        if (c.format != IVFPQ_KV_INT4) {
+            uint4* at = reinterpret_cast<uint4*>(values ? c.v + 2 * (page * c.vs[0] + head * c.vs[1] + t * c.vs[2] + e)
+                                                        : c.k + 2 * (page * c.ks[0] + head * c.ks[1] + t * c.ks[2] + e));
+            if (fresh) *at = now;
+            else now = *at;
+            if (full) unpack8<BF>(now, x);
+        } else {
+            uint8_t* rec = record_of(c, page, head, t / kTile);
+            const int tt = t % kTile, g = e / 64;
+            uint32_t* word = reinterpret_cast<uint32_t*>(rec + (values ? value_word(D, tt, e) : key_word(D, tt, e)));
+            __half* par = reinterpret_cast<__half*>(rec + (values ? value_param(D, tt, g) : key_param(D, tt, g)));
+            if (fresh) {
+                float s, z;
+                quantize8<BF>(now, word, &s, &z, x);
+                if (lane % 8 == 0) {
+                    if (values) {
+                        par[0] = __float2half_rn(s);
+                        par[2] = __float2half_rn(z);
+                    } else {
+                        *reinterpret_cast<__half2*>(par) = __floats2half2_rn(s, z);
                     }
-                } else {
-                    decode8(*kw, __half2float(ks[0]), __half2float(ks[1]), x);
                 }
+            } else {
+                decode8(*word, __half2float(par[0]), __half2float(par[1]), x);      // an older key
             }
-            if (full) {
+        }
+        if (full) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    hi[i] = fmaxf(hi[i], x[i]);
-                    lo[i] = fminf(lo[i], x[i]);
-                }
+            for (int i = 0; i < 8; ++i) {
+                hi[i] = fmaxf(hi[i], x[i]);
+                lo[i] = fminf(lo[i], x[i]);
             }
         }
     }
@@ -188,41 +181,53 @@ __global__ void __launch_bounds__(kThreads) append_kernel(Cache c, Batch b, Rows
     if (threadIdx.x == 0) c.scale[(int64_t)page * c.nheads + head] = __fmul_rn(top, 1.f / 127.f);
 }
 
-// 8 elements of one (token, head) per thread.
+constexpr int kReadTokens = 64;               // of a CTA
+
+// One head of 64 tokens per CTA, 8 elements of a token per thread and pass; the request is looked up where it changes, not per token.
 template <int D, bool BF>
 __global__ void __launch_bounds__(256) read_kernel(Cache c, Batch b, char* k, char* v, int* status) {
-    const int tok = blockIdx.x * (256 / (D / 8)) + threadIdx.x / (D / 8), head = blockIdx.y, e = threadIdx.x % (D / 8) * 8;
-    if (tok >= b.ntok) return;
-    const int r = request_of(b, tok);
-    const int2 mine = tokens_of(b, r, status);
-    const int len = length_of(b, c, r, status);
-    const int pos = len - mine.y + (tok - mine.x);
-    uint4 wk = make_uint4(0, 0, 0, 0), wv = wk;
-    if (pos >= 0 && pos < len) {
-        const int page = page_of(b, c, r, pos >> c.page_shift, status);
-        const int t = pos & (c.page - 1);
-        if (page >= 0) {
-            if (c.format != IVFPQ_KV_INT4) {
-                wk = *reinterpret_cast<const uint4*>(c.k + 2 * (page * c.ks[0] + head * c.ks[1] + t * c.ks[2] + e));
-                wv = *reinterpret_cast<const uint4*>(c.v + 2 * (page * c.vs[0] + head * c.vs[1] + t * c.vs[2] + e));
-            } else {
-                const uint8_t* rec = record_of(c, page, head, t / kTile);
-                const int tt = t % kTile, g = e / 64;
-                const __half* kp = reinterpret_cast<const __half*>(rec + key_param(D, tt, g));
-                const __half* vp = reinterpret_cast<const __half*>(rec + value_param(D, tt, g));
-                const uint32_t kw = *reinterpret_cast<const uint32_t*>(rec + key_word(D, tt, e));
-                const uint32_t vw = *reinterpret_cast<const uint32_t*>(rec + value_word(D, tt, e));
-                float x[8];
-                decode8(kw, __half2float(kp[0]), __half2float(kp[1]), x);
-                wk = pack8<BF>(x);
-                decode8(vw, __half2float(vp[0]), __half2float(vp[2]), x);
-                wv = pack8<BF>(x);
+    constexpr int kLanes = D / 8, kPass = 256 / kLanes;
+    const int head = blockIdx.y, e = threadIdx.x % kLanes * 8;
+    int end = 0, shift = 0, len = 0;              // of the thread's present request: its tokens' end, position minus token, tokens held
+    int r = -1;
+    for (int i = threadIdx.x / kLanes; i < kReadTokens; i += kPass) {
+        const int tok = blockIdx.x * kReadTokens + i;
+        if (tok >= b.ntok) return;
+        if (r < 0 || tok >= end) {
+            r = request_of(b, tok);
+            const int2 mine = tokens_of(b, r, status);
+            len = length_of(b, c, r, status);
+            end = mine.x + mine.y;
+            shift = len - mine.y - mine.x;
+        }
+        const int pos = tok + shift;
+        uint4 wk = make_uint4(0, 0, 0, 0), wv = wk;
+        if (pos >= 0 && pos < len) {
+            const int page = page_of(b, c, r, pos >> c.page_shift, status);
+            const int t = pos & (c.page - 1);
+            if (page >= 0) {
+                if (c.format != IVFPQ_KV_INT4) {
+                    wk = *reinterpret_cast<const uint4*>(c.k + 2 * (page * c.ks[0] + head * c.ks[1] + t * c.ks[2] + e));
+                    wv = *reinterpret_cast<const uint4*>(c.v + 2 * (page * c.vs[0] + head * c.vs[1] + t * c.vs[2] + e));
+                } else {
+                    const uint8_t* rec = record_of(c, page, head, t / kTile);
+                    const int tt = t % kTile, g = e / 64;
+                    const __half2 kp = *reinterpret_cast<const __half2*>(rec + key_param(D, tt, g));
+                    const __half* vp = reinterpret_cast<const __half*>(rec + value_param(D, tt, g));
+                    const uint32_t kw = *reinterpret_cast<const uint32_t*>(rec + key_word(D, tt, e));
+                    const uint32_t vw = *reinterpret_cast<const uint32_t*>(rec + value_word(D, tt, e));
+                    float x[8];
+                    decode8(kw, __low2float(kp), __high2float(kp), x);
+                    wk = pack8<BF>(x);
+                    decode8(vw, __half2float(vp[0]), __half2float(vp[2]), x);
+                    wv = pack8<BF>(x);
+                }
             }
         }
+        const int64_t at = ((int64_t)tok * c.nheads + head) * kLanes + e / 8;
+        reinterpret_cast<uint4*>(k)[at] = wk;
+        reinterpret_cast<uint4*>(v)[at] = wv;
     }
-    const int64_t i = ((int64_t)tok * c.nheads + head) * (D / 8) + e / 8;
-    reinterpret_cast<uint4*>(k)[i] = wk;
-    reinterpret_cast<uint4*>(v)[i] = wv;
 }
 
 // 4 channels of one (page, head) per thread.
@@ -265,15 +270,14 @@ void by_type(int d, bool bf16, F f) {
 
 cudaError_t launch_append(const Cache& c, const Batch& b, bool bf16, const Rows& k, const Rows& v, int* status, cudaStream_t st) {
     const int items = b.start ? (b.ntok >> c.page_shift) + 2 * b.nreq : b.nreq;
-    const dim3 grid(items, c.nheads);
+    const dim3 grid(items, c.nheads, 2);
     auto go = [&](auto d, auto bf) { append_kernel<decltype(d)::value, decltype(bf)::value><<<grid, kThreads, 0, st>>>(c, b, k, v, status); };
     by_type(c.d, bf16, go);
     return cudaGetLastError();
 }
 
 cudaError_t launch_read(const Cache& c, const Batch& b, bool bf16, char* k, char* v, int* status, cudaStream_t st) {
-    const int per = 256 / (c.d / 8);              // tokens of a CTA
-    const dim3 grid((b.ntok + per - 1) / per, c.nheads);
+    const dim3 grid((b.ntok + kReadTokens - 1) / kReadTokens, c.nheads);
     auto go = [&](auto d, auto bf) { read_kernel<decltype(d)::value, decltype(bf)::value><<<grid, 256, 0, st>>>(c, b, k, v, status); };
     by_type(c.d, bf16, go);
     return cudaGetLastError();
