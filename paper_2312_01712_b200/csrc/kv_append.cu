@@ -8,6 +8,7 @@ namespace kv {
 namespace {
 
 constexpr int kThreads = 128;
+__host__ __device__ constexpr int min_of(int a, int b) { return a < b ? a : b; }
 
 // Codes of 8 consecutive elements of a group of 64, spread over 8 neighbouring lanes, to *word; scale, offset and the held values.
 // The code is rint of the correctly rounded quotient (x - z) / s.  A product with the reciprocal differs from the quotient by less
@@ -104,48 +105,71 @@ __global__ void __launch_bounds__(kThreads) append_kernel(Cache c, Batch b, Rows
     }
     const Rows& in = values ? v : k;
     const char* src = in.p + 2 * ((int64_t)(tok.x + p0 - (len - tok.y)) * in.ts + (int64_t)head * in.hs + e);      // of token 0 of the block
-    auto load = [&](int t) -> uint4 {             // the next pass's elements, while this one's are worked on
-        return t < t_end && p0 + t >= first ? __ldg(reinterpret_cast<const uint4*>(src + 2 * t * in.ts)) : make_uint4(0, 0, 0, 0);
+    const int64_t step = 2 * (int64_t)kRows * in.ts;
+    auto bound = [&](const float* x) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            hi[i] = fmaxf(hi[i], x[i]);
+            lo[i] = fminf(lo[i], x[i]);
+        }
     };
-    uint4 next = load(t_begin + row);
-    for (int t0 = t_begin; t0 < t_end; t0 += kRows) {
-        const int t = t0 + row;
-        uint4 now = next;
-        next = load(t + kRows);
-        if (t >= t_end) continue;                 // whole groups of kLanes lanes
-        const bool fresh = p0 + t >= first;
-        float x[8];
-        if (c.format != IVFPQ_KV_INT4) {
-            uint4* at = reinterpret_cast<uint4*>(values ? c.v + 2 * (page * c.vs[0] + head * c.vs[1] + t * c.vs[2] + e)
-                                                        : c.k + 2 * (page * c.ks[0] + head * c.ks[1] + t * c.ks[2] + e));
-            if (fresh) *at = now;
-            else now = *at;
-            if (full) unpack8<BF>(now, x);
-        } else {
-            uint8_t* rec = record_of(c, page, head, t / kTile);
-            const int tt = t % kTile, g = e / 64;
-            uint32_t* word = reinterpret_cast<uint32_t*>(rec + (values ? value_word(D, tt, e) : key_word(D, tt, e)));
-            __half* par = reinterpret_cast<__half*>(rec + (values ? value_param(D, tt, g) : key_param(D, tt, g)));
-            if (fresh) {
-                float s, z;
-                quantize8<BF>(now, word, &s, &z, x);
-                if (lane % 8 == 0) {
-                    if (values) {
-                        par[0] = __float2half_rn(s);
-                        par[2] = __float2half_rn(z);
-                    } else {
-                        *reinterpret_cast<__half2*>(par) = __floats2half2_rn(s, z);
-                    }
-                }
+    if (c.format != IVFPQ_KV_INT4) {
+        const int64_t ts = values ? c.vs[2] : c.ks[2];
+        char* at = (values ? c.v + 2 * (page * c.vs[0] + head * c.vs[1] + e) : c.k + 2 * (page * c.ks[0] + head * c.ks[1] + e)) + 2 * (t_begin + row) * ts;
+        src += 2 * (t_begin + row) * in.ts;
+        for (int t = t_begin + row; t < t_end; t += kRows, at += 2 * kRows * ts, src += step) {
+            uint4 w;
+            if (p0 + t >= first) {
+                w = __ldg(reinterpret_cast<const uint4*>(src));
+                *reinterpret_cast<uint4*>(at) = w;
             } else {
-                decode8(*word, __half2float(par[0]), __half2float(par[1]), x);      // an older key
+                w = *reinterpret_cast<const uint4*>(at);
+            }
+            if (full) {
+                float x[8];
+                unpack8<BF>(w, x);
+                bound(x);
             }
         }
-        if (full) {
+    } else {
+        // record by record, its tokens in 16 / kRows passes: all offsets but the record's own are constants.  The next pass's elements are
+        // on their way while this one's are worked on.
+        constexpr int kPasses = kTile / kRows;
+        const int r0 = t_begin / kTile * kTile, g = e / 64;
+        uint8_t* rec = record_of(c, page, head, r0 / kTile) ;
+        uint8_t* word = rec + (values ? value_word(D, row, e) : key_word(D, row, e));
+        uint8_t* par = rec + (values ? value_param(D, row, g) : key_param(D, row, g));
+        src += 2 * (r0 + row) * in.ts;
+        auto load = [&](int t) -> uint4 { return t >= t_begin && t < t_end && p0 + t >= first ? __ldg(reinterpret_cast<const uint4*>(src)) : make_uint4(0, 0, 0, 0); };
+        uint4 next = load(r0 + row);
+        for (int t0 = r0; t0 < t_end; t0 += kTile, word += 18 * D, par += 18 * D) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                hi[i] = fmaxf(hi[i], x[i]);
-                lo[i] = fminf(lo[i], x[i]);
+            for (int u = 0; u < kPasses; ++u) {
+                const int t = t0 + u * kRows + row;
+                const uint4 now = next;
+                src += step;
+                next = load(t + kRows);
+                if (t < t_begin || t >= t_end) continue;      // whole groups of kLanes lanes
+                // what the pass adds to the offsets of token `row`
+                constexpr int kKeyWord = kRows * min_of(D, 128) / 2, kKeyPar = kRows * (D / 64) * 4;
+                uint32_t* w = reinterpret_cast<uint32_t*>(word + (values ? value_word(D, u * kRows, 0) - value_word(D, 0, 0) : u * kKeyWord));
+                __half* q = reinterpret_cast<__half*>(par + (values ? value_param(D, u * kRows, 0) - value_param(D, 0, 0) : u * kKeyPar));
+                float x[8];
+                if (p0 + t >= first) {
+                    float s, z;
+                    quantize8<BF>(now, w, &s, &z, x);
+                    if (lane % 8 == 0) {
+                        if (values) {
+                            q[0] = __float2half_rn(s);
+                            q[2] = __float2half_rn(z);
+                        } else {
+                            *reinterpret_cast<__half2*>(q) = __floats2half2_rn(s, z);
+                        }
+                    }
+                } else {
+                    decode8(*w, __half2float(q[0]), __half2float(q[1]), x);      // an older key
+                }
+                if (full) bound(x);
             }
         }
     }
