@@ -25,12 +25,18 @@ namespace kv {
 namespace {
 
 constexpr int kMaxCtas = 640;            // CTAs that share work (tickets and partial results in the workspace)
+// FMT of an instance: a cache's IVFPQ_KV_* format, for queries and results in bf16 (or in the cache's own type), or
+constexpr int kInt4Half = 3;             // 4 bits with queries and results in fp16
 // Shape of an instance.
-template <int FMT, int D, int NT>
+template <int FMT, int D, int NT, bool LIST>
 struct Shape {
-    static constexpr bool kInt4 = FMT == IVFPQ_KV_INT4;
+    static constexpr bool kInt4 = FMT == IVFPQ_KV_INT4 || FMT == kInt4Half;
+    static constexpr bool kBf16 = FMT == IVFPQ_KV_INT4 || FMT == IVFPQ_KV_BF16;      // queries and results
+    static constexpr bool kFine = FMT == kInt4Half;    // p in two fp16 numbers: see there
     static constexpr int kRows = 8 * NT;
-    static constexpr int kWarps = kInt4 ? 8 : 4;
+    // 4 bits: 8 warps a CTA halve the parts of a long cache that have to be joined (100 003 tokens x 8 heads: 41 us, 4 warps 53 us); lists are
+    // short, and small CTAs let one's start and end hide behind another's keys (2048 tokens x 8 heads x 1024 keys: 547 us, 8 warps 668 us)
+    static constexpr int kWarps = kInt4 && !LIST ? 8 : 4;
     static constexpr int kThreads = 32 * kWarps;
     static constexpr int kUnit = 32 * kWarps;          // keys of a unit: 32 per warp
     static constexpr int kStageKeys = kInt4 ? 32 : 16;
@@ -39,7 +45,7 @@ struct Shape {
     static constexpr int kStages = D == 64 ? 4 : 3;
     static constexpr int kRingBytes = kStages * kStageBytes;
     static constexpr int kSmem = kWarps * kRingBytes;
-    static constexpr int kMinCtas = kInt4 ? (D == 64 || (D == 128 && NT == 1) ? 2 : 1) : (D == 256 ? 1 : 2);
+    static constexpr int kMinCtas = kInt4 ? (D == 64 || (D == 128 && NT == 1) ? 2 : 1) * (8 / kWarps) : (D == 256 ? 1 : 2);
     static_assert(kRingBytes >= kRows * (D + 4) * 4, "a warp's ring holds its O");
 };
 
@@ -94,8 +100,8 @@ __device__ __forceinline__ bool tile_of(const AttendArgs& a, const Plan& p, int 
 
 // P16: 4-bit pages of 16 tokens, whose records of a stage lie apart.
 template <int FMT, int D, int NT, bool LIST, bool P16>
-__global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, NT>::kMinCtas)) attend_kernel(AttendArgs a, Plan plan) {
-    using S = Shape<FMT, D, NT>;
+__global__ void __launch_bounds__((Shape<FMT, D, NT, LIST>::kThreads), (Shape<FMT, D, NT, LIST>::kMinCtas)) attend_kernel(AttendArgs a, Plan plan) {
+    using S = Shape<FMT, D, NT, LIST>;
     constexpr bool kInt4 = S::kInt4;
     constexpr bool BF = FMT == IVFPQ_KV_BF16;
     constexpr int R = S::kRows, G = D / 64, KSTEPS = D / 16, MT = D / 16;
@@ -435,13 +441,8 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
             } else {
                 // scaled by a power of two to just below 2^15
                 float x[G][2][8], top = 0.f;
-                if (a.bf16) {
 #pragma unroll
-                    for (int i = 0; i < 2 * G; ++i) unpack8<true>(raw[nt][i / 2][i % 2], x[i / 2][i % 2]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 2 * G; ++i) unpack8<false>(raw[nt][i / 2][i % 2], x[i / 2][i % 2]);
-                }
+                for (int i = 0; i < 2 * G; ++i) unpack8<S::kBf16>(raw[nt][i / 2][i % 2], x[i / 2][i % 2]);
 #pragma unroll
                 for (int i = 0; i < 16 * G; ++i) top = fmaxf(top, fabsf(x[i / 16][i / 8 % 2][i % 8]));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -623,7 +624,9 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
                         }
                     }
             }
-            uint32_t pf[S::kSubs][NT][2];
+            // fp16 results over a 4-bit cache: the value's rounding and p's would together weigh 1.4 times the result's own (relative 3.4e-4 against
+            // 2.1e-4 of a result that is only rounded at its end), so what rounding p leaves over enters as a second product
+            uint32_t pf[S::kSubs][NT][2], p_rest[S::kSubs][NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
@@ -633,8 +636,14 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
                     const float e2 = ex2(fmaf(p[i][nt][2], cf[nt][0], -m0)), e3 = ex2(fmaf(p[i][nt][3], cf[nt][1], -m1));
                     l[nt][0] += e0 + e2;
                     l[nt][1] += e1 + e3;
-                    pf[i][nt][0] = movmatrix(pack2<BF>(e0, e1));
-                    pf[i][nt][1] = movmatrix(pack2<BF>(e2, e3));
+                    const uint32_t h0 = pack2<BF>(e0, e1), h1 = pack2<BF>(e2, e3);
+                    pf[i][nt][0] = movmatrix(h0);
+                    pf[i][nt][1] = movmatrix(h1);
+                    if (S::kFine) {
+                        const float2 r0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), r1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+                        p_rest[i][nt][0] = movmatrix(pack2<BF>(e0 - r0.x, e1 - r0.y));
+                        p_rest[i][nt][1] = movmatrix(pack2<BF>(e2 - r1.x, e3 - r1.y));
+                    }
                 }
             }
 
@@ -693,7 +702,10 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
                                     }
                                     const int mt = pl * (DP / 16) + wi * 4 + hf * 2 + q;
 #pragma unroll
-                                    for (int nt = 0; nt < NT; ++nt) mma16816<false>(o[mt][nt], f[0], f[1], f[2], f[3], pf[i][nt][0], pf[i][nt][1]);
+                                    for (int nt = 0; nt < NT; ++nt) {
+                                        mma16816<false>(o[mt][nt], f[0], f[1], f[2], f[3], pf[i][nt][0], pf[i][nt][1]);
+                                        if (S::kFine) mma16816<false>(o[mt][nt], f[0], f[1], f[2], f[3], p_rest[i][nt][0], p_rest[i][nt][1]);
+                                    }
                                 }
                             }
                     }
@@ -745,7 +757,7 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
             const int rr = tl.row0 + row, j = rr / a.group, g = rr % a.group;
             const int64_t orow = (int64_t)(tl.tok0 + j) * (c.nheads * a.group) + head * a.group + g;
             const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
-            const bool bf = a.bf16;
+            constexpr bool bf = S::kBf16;
             uint2 w;
             const bool nan = lsum != lsum;
             float y[4];
@@ -873,7 +885,7 @@ __global__ void __launch_bounds__((Shape<FMT, D, NT>::kThreads), (Shape<FMT, D, 
 
 template <int FMT, int D, int NT, bool LIST, bool P16>
 cudaError_t run(const AttendArgs& a, int sms, cudaStream_t st) {
-    using S = Shape<FMT, D, NT>;
+    using S = Shape<FMT, D, NT, LIST>;
     constexpr int R = S::kRows;
     auto kernel = attend_kernel<FMT, D, NT, LIST, P16>;
     static int known[64];                     // per instance and device: CTAs an SM holds
@@ -915,10 +927,10 @@ cudaError_t pick_rows(const AttendArgs& a, int sms, cudaStream_t st) {
     const bool list = a.blocks != nullptr;
     // rows that can share a kv head: one token's query heads, or those of several tokens of a request
     // (4 bits at d = 256 take 8 rows at a time: 16 leave the key loop too few registers, 16 requests of 8000 tokens x 4 heads, group 16: 84 us against 67)
-    const bool wide = !(FMT == IVFPQ_KV_INT4 && D == 256) && (a.group > 8 || (!list && a.b.start != nullptr));
-    constexpr int W = FMT == IVFPQ_KV_INT4 && D == 256 ? 1 : 2;
-    if (FMT == IVFPQ_KV_INT4 && a.c.page == 16) {
-        constexpr bool P = FMT == IVFPQ_KV_INT4;
+    const bool wide = !(Shape<FMT, D, 1, false>::kInt4 && D == 256) && (a.group > 8 || (!list && a.b.start != nullptr));
+    constexpr int W = Shape<FMT, D, 1, false>::kInt4 && D == 256 ? 1 : 2;
+    if (Shape<FMT, D, 1, false>::kInt4 && a.c.page == 16) {
+        constexpr bool P = Shape<FMT, D, 1, false>::kInt4;
         if (list) return wide ? run<FMT, D, W, true, P>(a, sms, st) : run<FMT, D, 1, true, P>(a, sms, st);
         return wide ? run<FMT, D, W, false, P>(a, sms, st) : run<FMT, D, 1, false, P>(a, sms, st);
     }
@@ -943,7 +955,7 @@ cudaError_t launch_attend(const AttendArgs& a, cudaStream_t st) {
     int sms = 0;
     const cudaError_t e = sm_count(&sms);
     if (e != cudaSuccess) return e;
-    if (a.c.format == IVFPQ_KV_INT4) return pick_width<IVFPQ_KV_INT4>(a, sms, st);
+    if (a.c.format == IVFPQ_KV_INT4) return a.bf16 ? pick_width<IVFPQ_KV_INT4>(a, sms, st) : pick_width<kInt4Half>(a, sms, st);
     if (a.c.format == IVFPQ_KV_BF16) return pick_width<IVFPQ_KV_BF16>(a, sms, st);
     return pick_width<IVFPQ_KV_FP16>(a, sms, st);
 }
