@@ -178,15 +178,18 @@ def ivfpq_kv_read(cache: KvCacheHandle, batch: KvBatchHandle, ntok: int, dtype: 
     """The held keys and values of the step's `ntok` tokens, each [tokens, heads, d]."""
     if out is None:
         dtype = dtype or cache.dtype or torch.bfloat16
-        out = tuple(cache._any.new_empty((ntok, cache.nheads, cache.d), dtype=dtype) for _ in range(2))
-    k, v = out
-    if k.shape[0] != ntok:
-        raise ValueError("out must have ntok rows")
-    dt = _rows(k, cache, "out[0]")
-    if _rows(v, cache, "out[1]") != dt or k.shape != v.shape or k.shape[1] != cache.nheads or not k.is_contiguous() or not v.is_contiguous():
-        raise ValueError("out must be two contiguous tensors [tokens, kv heads, d] of one type")
+        if dtype not in _FORMAT:
+            raise ValueError("dtype must be bf16 or fp16")
+        k, v = cache._any.new_empty((2, ntok, cache.nheads, cache.d), dtype=dtype).unbind(0)      # one allocation
+        dt = _FORMAT[dtype]
+    else:
+        k, v = out
+        dt = _rows(k, cache, "out[0]")
+        if _rows(v, cache, "out[1]") != dt or k.shape != v.shape or k.shape[:2] != (ntok, cache.nheads) or not k.is_contiguous() \
+                or not v.is_contiguous():
+            raise ValueError("out must be two contiguous tensors [ntok, kv heads, d] of one type")
     stream, ws = cache._call()
-    _check(_load().ivfpq_kv_read(cache._ref, batch._ref, k.shape[0], dt, k.data_ptr(), v.data_ptr(), ws, cache._nbytes, stream),
+    _check(_load().ivfpq_kv_read(cache._ref, batch._ref, ntok, dt, k.data_ptr(), v.data_ptr(), ws, cache._nbytes, stream),
            "ivfpq_kv_read")
     return k, v
 
@@ -197,9 +200,10 @@ def ivfpq_kv_read_bounds(cache: KvCacheHandle, pages: torch.Tensor):
         raise ValueError("pages must be a contiguous int32 tensor on the cache's device")
     if cache.bounds is None:
         raise ValueError("the cache keeps no bounds")
-    hi, lo = (cache.bounds_scale.new_empty((pages.shape[0], cache.nheads, cache.d)) for _ in range(2))
+    n = pages.shape[0]
+    hi, lo = cache.bounds_scale.new_empty((2, n, cache.nheads, cache.d)).unbind(0)
     stream, ws = cache._call()
-    _check(_load().ivfpq_kv_read_bounds(cache._ref, pages.data_ptr(), pages.shape[0], hi.data_ptr(), lo.data_ptr(), ws, cache._nbytes,
+    _check(_load().ivfpq_kv_read_bounds(cache._ref, pages.data_ptr(), n, hi.data_ptr(), lo.data_ptr(), ws, cache._nbytes,
                                         stream), "ivfpq_kv_read_bounds")
     return hi, lo
 
