@@ -72,7 +72,8 @@ class KvCacheHandle:
     """A paged key/value cache on tensors of the caller's: `records` uint8 [pages, heads, page / 16, 18 * d]
     (4 bits) or `k` and `v` [pages, heads, page, d] (bf16 or fp16, any strides with the last axis contiguous);
     `bounds` int8 [pages, heads, 2, d] and `bounds_scale` fp32 [pages, heads] if blocks are to be selected.
-    One workspace per stream that calls are made on belongs to the handle."""
+    One workspace per stream that calls are made on belongs to the handle; graphs captured on one stream share that
+    stream's, so their replays must not overlap."""
 
     def __init__(self, records: Optional[torch.Tensor] = None, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
                  bounds: Optional[torch.Tensor] = None, bounds_scale: Optional[torch.Tensor] = None):
@@ -110,6 +111,11 @@ class KvCacheHandle:
         if self._nbytes == 0 or s.page not in (16, 32, 64, 128):
             raise IvfpqError(IVFPQ_ERR_UNSUPPORTED, "KvCacheHandle")
         self._ws: dict = {}
+        self._spare = None
+        if not torch.cuda.is_current_stream_capturing():
+            # for a stream whose first call is captured: what that call did to the workspace would be done by replays only
+            self._spare = self._zeroed()
+            torch.cuda.current_stream(self.device).synchronize()
         self._at: dict = {}          # addresses of the workspaces
         self._index = first.device.index
 
@@ -124,12 +130,22 @@ class KvCacheHandle:
                    v=torch.zeros(npages, nheads, page, d, dtype=dtype, device=device), **b)
 
     def workspace(self, stream: int) -> torch.Tensor:
-        """The workspace of calls on `stream`: calls on two streams may overlap, so each has its own."""
+        """The workspace of calls on `stream`: calls on two streams may overlap, so each has its own.  The first call on a
+        stream may be captured for one stream of a handle; others need a call before the capture."""
         ws = self._ws.get(stream)
         if ws is None:
-            ws = torch.empty(self._nbytes, dtype=torch.uint8, device=self.device)
-            ws[:IVFPQ_KV_WORKSPACE_ZERO].zero_()
+            if not torch.cuda.is_current_stream_capturing():
+                ws = self._zeroed()
+            elif self._spare is not None:
+                ws, self._spare = self._spare, None
+            else:
+                raise RuntimeError("the cache has no workspace for this stream yet: make one call on it before capturing")
             self._ws[stream] = ws
+        return ws
+
+    def _zeroed(self) -> torch.Tensor:
+        ws = torch.empty(self._nbytes, dtype=torch.uint8, device=self.device)
+        ws[:IVFPQ_KV_WORKSPACE_ZERO].zero_()
         return ws
 
     def _call(self) -> Tuple[int, int]:

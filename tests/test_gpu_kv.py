@@ -492,6 +492,32 @@ def test_calls_on_two_streams_and_in_a_graph():
     assert torch.equal(out, lib.ivfpq_kv_attend(s.cache, s.batch, q))
 
 
+def test_a_first_call_on_a_stream_may_be_captured():
+    s = Setup("int4", "bf16", hkv=2, lens=(9000, 40, 2500), seed=8, page=128)
+    want = lib.ivfpq_kv_attend(s.cache, s.batch, s.q)
+    q = s.q.contiguous()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    outs, graphs = [torch.zeros_like(want), torch.zeros_like(want)], [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    torch.cuda.synchronize()
+    for out, g in zip(outs, graphs):                           # two graphs of one stream that had no call before
+        with torch.cuda.graph(g, stream=streams[0]):
+            lib.ivfpq_kv_attend(s.cache, s.batch, q, out=out)
+    assert not s.cache._ws[streams[0].cuda_stream][:lib.IVFPQ_KV_WORKSPACE_ZERO].any()      # zeroed before any replay
+    with torch.cuda.stream(streams[0]):                        # a plain call, then the graphs in the other order
+        plain = lib.ivfpq_kv_attend(s.cache, s.batch, q)
+    torch.cuda.synchronize()
+    graphs[1].replay()
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    assert torch.equal(plain, want) and torch.equal(outs[0], want) and torch.equal(outs[1], want)
+    g = torch.cuda.CUDAGraph()
+    with pytest.raises(RuntimeError, match="before capturing"):
+        with torch.cuda.graph(g, stream=streams[1]):
+            lib.ivfpq_kv_attend(s.cache, s.batch, q, out=outs[0])
+    with torch.cuda.stream(streams[1]):
+        assert torch.equal(lib.ivfpq_kv_attend(s.cache, s.batch, q), want)
+
+
 def test_the_binding_checks_tensors_and_the_first_use_of_select_needs_bounds():
     s = Setup("bf16", "bf16", lens=(100, 50))
     with pytest.raises(ValueError):
